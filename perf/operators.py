@@ -1,0 +1,490 @@
+"""Performance cases of the cache operators that a server of speculation windows runs around the verification step: new
+rows into the paged cache (norms of queries and keys, position rotation), attention of the windows' rows over it (single
+tokens, chains, draft trees, a sliding window with sinks), the masks of draft trees, and keeping the accepted path.
+
+``own`` chooses between the framework's entry points and their plain form in elementary torch operations.  Sizes are those
+of the synthetic verification workloads (8B- and 70B-shaped targets: 32 or 64 query heads, 8 heads of keys and values, 128
+elements each) and generic ones beside them.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEVICE = "cuda:0"
+EPS = 1e-5
+SINKS = 4
+
+
+def _case(name, op, B, K, n_q=32, n_kv=8, D=128, dtype="bf16", kv="same", page=16, lo=0, hi=256, **more):
+    """lo, hi: the cached lengths run from one to the other over the windows."""
+    return dict(name=name, op=op, B=B, K=K, n_q=n_q, n_kv=n_kv, D=D, dtype=dtype, kv=kv, page=page, lo=lo, hi=hi, **more)
+
+
+def listed():
+    return [
+        # one new token of an 8B-class target: launch and latency are all there is
+        _case("append_8b_b1", "append", 1, 0, rot=128, hi=700, lo=700),
+        # the widest batch of windows of a 70B-class target, queries, keys and values in one row of a fused projection
+        _case("append_70b_b128_k64", "append", 128, 64, 64, rot=128, fused=True, lo=3, hi=300),
+        # single-token decoding at batch 1: the cache is split over the whole chip
+        _case("decode_8b_b1", "attend", 1, 0, lo=2500, hi=2500),
+        # single-token decoding of a ragged batch, a few tokens to 8192
+        _case("decode_70b_b64", "attend", 64, 0, 64, lo=17, hi=8192),
+        # draft trees of 32 nodes over an FP8 cache of up to 16384 tokens
+        _case("tree_70b_b8_k32_fp8", "attend", 8, 32, 64, kv="fp8", page=64, lo=2000, hi=16384, tree=True),
+        # chains of 64 draft tokens for 128 windows: bound by the matrix pipe
+        _case("verify_70b_b128_k64", "attend", 128, 64, 64, lo=500, hi=3500),
+        # short windows over long contexts of which the last 4096 tokens and the sinks are visible
+        _case("window_8b_b16_k7", "attend", 16, 7, window=4096, page=32, lo=1000, hi=65000),
+        # a piece of a prompt in fp32, a small model's heads, ragged row counts
+        _case("window_f32_b2_k255", "attend", 2, 255, 16, 16, 64, "f32", window=200, lo=0, hi=777, ragged=True),
+        # masks of one draft tree, and of many large ones
+        _case("mask_b1_k32", "mask", 1, 32),
+        _case("mask_b128_k500", "mask", 128, 500),
+        # the accepted path of one small tree in 32 layers; of 128 trees in 16 layers
+        _case("commit_8b_b1_k16", "commit", 1, 16, layers=32, lo=90, hi=90),
+        _case("commit_70b_b128_k64", "commit", 128, 64, 64, layers=16, lo=1, hi=200),
+    ]
+
+
+def _log_uniform(rng, a, b):
+    return math.exp(rng.uniform(math.log(a), math.log(b)))
+
+
+def draw(rng):
+    op = rng.choice(["append", "attend", "attend", "attend", "attend", "mask", "commit"])
+    dtype, kv = rng.choice([("bf16", "same"), ("bf16", "same"), ("bf16", "same"), ("bf16", "fp8"), ("f32", "same")])
+    n_kv = rng.choice([1, 2, 4, 8, 8, 8, 16])
+    n_q = n_kv * rng.choice([1, 2, 4, 4, 7, 8, 8])
+    D = rng.choice([64, 128, 128, 128, 96, 80, 256])
+    page = rng.choice([1, 8, 16, 16, 32, 64, 256])
+    B = int(_log_uniform(rng, 1, 129))
+    K = rng.choice([0, 0, int(_log_uniform(rng, 1, 65)), int(_log_uniform(rng, 1, 65)), int(_log_uniform(rng, 64, 513))])
+    more = {}
+    lo, hi = sorted(int(_log_uniform(rng, 1, 300)) - 1 for _ in range(2))
+    if op == "append":
+        while B * (K + 1) * (n_q + 2 * n_kv) * D * (4 if dtype == "f32" else 2) > 1.5e8:
+            B, K = (B + 1) // 2, K // 2
+        more = dict(rot=rng.choice([D, D, D // 32 * 16]), style=rng.choice(["half", "half", "interleaved"]), norm=rng.random() < 0.7,
+                    fused=rng.random() < 0.5, tree=K > 0 and rng.random() < 0.3, ragged=rng.random() < 0.3)
+    elif op == "attend":
+        lo, hi = sorted(int(_log_uniform(rng, 1, 20000)) for _ in range(2))
+        more = dict(window=rng.choice([0, 0, int(_log_uniform(rng, 32, 4097))]), tree=K > 0 and rng.random() < 0.3, ragged=rng.random() < 0.2)
+        c = _case("", op, B, K, n_q, n_kv, D, dtype, kv, page, lo, hi, **more)
+        # below the largest listed cases: fp32 runs at a fraction of the bf16 rate, and the plain form holds all scores
+        while B * (K + 1) * n_q * (hi + K) > 1.0e9 or work(c)["flops"] > (3e10 if dtype == "f32" else 4e11) or B * (hi + K) * n_kv * D > 4e8:
+            if B > 1:
+                B = (B + 1) // 2
+            else:
+                hi, lo = (hi + 1) // 2, (lo + 1) // 2
+            c = _case("", op, B, K, n_q, n_kv, D, dtype, kv, page, lo, hi, **more)
+    elif op == "mask":
+        K = max(1, K) if rng.random() < 0.5 else int(_log_uniform(rng, 8, 501))
+        n_q, n_kv, D, dtype, kv, page, lo, hi = 32, 8, 128, "bf16", "same", 16, 0, 256
+    else:
+        K = max(1, min(K, 64))
+        more = dict(layers=int(_log_uniform(rng, 1, 81)))
+        while B * (K + hi + 2 + page) * more["layers"] * n_kv * D > 5e8:
+            B, more["layers"] = (B + 1) // 2, (more["layers"] + 1) // 2
+    case = _case("", op, B, K, n_q, n_kv, D, dtype, kv, page, lo, hi, **more)
+    del case["name"]
+    return case
+
+
+def _lengths(c):
+    """Cached tokens and live rows of every window; windows differ from neighbour to neighbour."""
+    B, K = c["B"], c["K"]
+    at = [(b * 0.6180339887498949) % 1.0 for b in range(B)]
+    lens = [c["lo"] + int(round((c["hi"] - c["lo"]) * (1.0 - a))) for a in at]
+    rows = [K + 1 if not c.get("ragged") else max(1 if b == 0 else 0, K + 1 - int((K + 2) * ((b * 0.3819660112501051) % 1.0))) for b in range(B)]
+    return lens, rows
+
+
+def work(c):
+    B, K, D, nq, nkv = c["B"], c["K"], c["D"], c["n_q"], c["n_kv"]
+    es = 4 if c["dtype"] == "f32" else 2
+    kes = 1 if c["kv"] == "fp8" else es
+    lens, rows = _lengths(c)
+    if c["op"] == "append":
+        n = sum(rows)
+        return {"bytes": n * D * (2 * nq * es + 2 * nkv * (es + kes)) + n * 4 + B * 8, "flops": n * 6.0 * D * (nq + nkv)}
+    if c["op"] == "mask":
+        return {"bytes": B * (4 * K + 4 * (K + 1) * (1 + (K + 32) // 32)), "flops": 0}
+    if c["op"] == "commit":
+        # a node hangs under one of the last three before it: about every other node is on the path, all but the first moved
+        moved = B * K // 2
+        return {"bytes": 4.0 * c["layers"] * moved * nkv * D * kes + B * (4 * K + 16), "flops": 0}
+    w = c.get("window", 0)
+    keys = pairs = 0
+    for L, n in zip(lens, rows):
+        seen = L + n                                                      # tokens that any row of the window sees
+        if w:
+            seen = min(seen, min(SINKS, L) + min(L, w - 1) + n)
+        keys += seen if n else 0
+        inner = n * (n + 1) // (4 if c.get("tree") else 2)                # new rows seen by new rows
+        pairs += n * L + inner if not w else min(n * L + inner, n * (w + SINKS))
+    return {"bytes": 2.0 * keys * nkv * D * kes + 2.0 * sum(rows) * nq * D * es, "flops": 4.0 * D * nq * pairs}
+
+
+# --- inputs ---------------------------------------------------------------------------------------------------------
+
+def _trees(c, g):
+    """Parents of draft trees: node j hangs under one of the three nodes before it, so that paths are long."""
+    B, K = c["B"], c["K"]
+    j = torch.arange(K, device=DEVICE)
+    back = 1 + (torch.rand(B, K, generator=g, device=DEVICE) * 3).long().clamp(max=2)
+    return (j - back).clamp(min=-1).to(torch.int32).contiguous()
+
+
+def _reach(parent):
+    """[B, K+1, K+1] of 0 and 1: row r has a 1 at itself and at its ancestors (row 0 is the root, row j+1 is node j)."""
+    B, K = parent.shape
+    up = torch.zeros(B, K + 1, K + 1, device=parent.device)
+    up.scatter_(2, torch.nn.functional.pad(parent.long() + 1, (1, 0))[:, :, None], 1.0)
+    up[:, 0, 0] = 0.0
+    # rows within one step of each other, squared until every distance is covered
+    reach = up + torch.eye(K + 1, device=parent.device)
+    for _ in range(K.bit_length()):
+        reach = (reach @ reach).clamp(max=1.0)
+    return reach
+
+
+def _pack(bits):
+    """[..., n] truth values -> [..., ceil(n/32)] int32 words, bit j of word w for place 32 w + j."""
+    n = bits.shape[-1]
+    x = torch.nn.functional.pad(bits.long(), (0, -n % 32)).unflatten(-1, (-1, 32))
+    x = (x << torch.arange(32, device=bits.device)).sum(-1)
+    return ((x ^ 0x80000000) - 0x80000000).to(torch.int32)
+
+
+class _Cache:
+    """A cache handle that goes away with the state that holds it."""
+
+    def __init__(self, c, width, pages, stride):
+        import paper_2504_20039_amd as aj
+
+        self.aj = aj
+        self.h = aj.aj_cache_create(
+            c["B"], c["K"], c["n_q"], c["n_kv"], c["D"], c["page"], pages, width, aj.AJ_F32 if c["dtype"] == "f32" else aj.AJ_BF16,
+            aj.AJ_KV_FP8_E4M3 if c["kv"] == "fp8" else aj.AJ_KV_SAME, window=c.get("window", 0), sinks=SINKS if c.get("window", 0) else 0,
+            rot_dim=c.get("rot", 0), rope=aj.AJ_ROPE_INTERLEAVED if c.get("style") == "interleaved" else aj.AJ_ROPE_HALF, qkv_stride=stride)
+
+    def __del__(self):
+        torch.cuda.synchronize()
+        self.aj.aj_cache_destroy(self.h)
+
+
+def prepare(c, seed):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(int(seed))
+    B, K, D, nq, nkv, page = c["B"], c["K"], c["D"], c["n_q"], c["n_kv"], c["page"]
+    R = K + 1
+    dt = torch.float32 if c["dtype"] == "f32" else torch.bfloat16
+
+    def normal(*shape, std=1.0, dtype=dt):
+        return torch.randn(*shape, generator=g, device=DEVICE, dtype=dtype).mul_(std)
+
+    s = dict(case=c)
+    if c["op"] == "mask" or c["op"] == "commit" or c.get("tree"):
+        s["parent"] = _trees(c, g)
+    if c["op"] == "mask":
+        s["depth"] = torch.zeros(B, R, dtype=torch.int32, device=DEVICE)
+        s["mask"] = torch.zeros(B, R, (R + 31) // 32, dtype=torch.int32, device=DEVICE)
+        return s
+
+    lens, rows = _lengths(c)
+    width = max(-(-(n + R) // page) for n in lens)
+    used = [-(-(n + R) // page) for n in lens]
+    pages = sum(used) + 3                       # a few pages of the pool belong to nobody
+    s["cache_len"] = torch.tensor(lens, dtype=torch.int32, device=DEVICE)
+    s["n_rows"] = torch.tensor(rows, dtype=torch.int32, device=DEVICE) if c.get("ragged") else None
+    order = torch.randperm(pages, generator=g, device=DEVICE).to(torch.int32)
+    first = torch.tensor([sum(used[:b]) for b in range(B)], device=DEVICE)
+    col = torch.arange(width, device=DEVICE)
+    table = order[(first[:, None] + col).clamp(max=pages - 1)]
+    s["table"] = torch.where(col < torch.tensor(used, device=DEVICE)[:, None], table, -1).to(torch.int32).contiguous()
+
+    scales = (0.03, 0.02) if c["kv"] == "fp8" else (1.0, 1.0)
+    s["k_scale"], s["v_scale"] = scales
+    lead = (c["layers"],) if c["op"] == "commit" else ()
+    pools = []
+    for scale in scales:
+        x = normal(*lead, pages, page, nkv, D)
+        pools.append((x.float() / scale).clamp(-448, 448).to(torch.float8_e4m3fn) if c["kv"] == "fp8" else x)
+        del x
+    s["k_pool"], s["v_pool"] = pools
+    s["depth"] = s["mask"] = None
+    if c.get("tree"):
+        reach = _reach(s["parent"])
+        s["depth"] = (reach.sum(2) - 1).to(torch.int32).contiguous()
+        s["mask"] = _pack(reach > 0.5).contiguous()
+
+    stride = 0
+    if c["op"] == "append":
+        if c.get("fused"):
+            stride = (nq + 2 * nkv) * D
+            s["q"], s["k"], s["v"] = normal(B, R, stride).split([nq * D, nkv * D, nkv * D], 2)
+        else:
+            s["q"], s["k"], s["v"] = normal(B, R, nq * D), normal(B, R, nkv * D), normal(B, R, nkv * D)
+        s["q_norm"], s["k_norm"] = [(1.0 + normal(D, std=0.1, dtype=torch.float32)).to(dt) for _ in range(2)] if c.get("norm", True) else (None, None)
+        rot = c["rot"]
+        s["inv_freq"] = (10000.0 ** (-torch.arange(0, rot, 2, device=DEVICE, dtype=torch.float64) / max(rot, 1))).float()
+        s["q_out"] = torch.zeros(B, R, nq * D, dtype=dt, device=DEVICE)
+    elif c["op"] == "attend":
+        # queries as trained models have them: most rows look at many tokens, some at few
+        s["q"] = (normal(B, R, nq, D, dtype=torch.float32) * torch.rand(B, R, nq, 1, generator=g, device=DEVICE).mul_(3.0)).to(dt).view(B, R, nq * D)
+        s["out"] = torch.zeros(B, R, nq * D, dtype=dt, device=DEVICE)
+        s["lse"] = torch.zeros(B, R, nq, dtype=torch.float32, device=DEVICE)
+    else:
+        # the accepted node: the deepest of the last few
+        s["out_node"] = (K - 1 - (torch.rand(B, generator=g, device=DEVICE) * min(3, K)).long()).clamp(min=0).to(torch.int32)
+        s["new_len"] = torch.zeros(B, dtype=torch.int32, device=DEVICE)
+    if own:
+        s["cache"] = _Cache(c, width, pages, stride)
+    return s
+
+
+# --- one pass -------------------------------------------------------------------------------------------------------
+
+def run(s):
+    return _run_own(s) if own else _run_plain(s)
+
+
+def _run_own(s):
+    import paper_2504_20039_amd as aj
+
+    c = s["case"]
+    if c["op"] == "mask":
+        aj.aj_tree_mask(c["B"], c["K"], s["parent"], s["depth"], s["mask"])
+        return {"depth": s["depth"], "mask": s["mask"]}
+    h = s["cache"].h
+    if c["op"] == "append":
+        aj.aj_cache_append(h, s["q"], s["k"], s["v"], s["q_norm"], s["k_norm"], EPS, s["inv_freq"], s["table"], s["cache_len"], s["q_out"],
+                           s["k_pool"], s["v_pool"], n_rows=s["n_rows"], depth=s["depth"], k_scale=s["k_scale"], v_scale=s["v_scale"])
+        return {"q": s["q_out"], "k_pool": s["k_pool"], "v_pool": s["v_pool"]}
+    if c["op"] == "commit":
+        aj.aj_cache_commit(h, s["parent"], s["out_node"], s["table"], s["cache_len"], c["layers"], s["k_pool"].stride(0), s["k_pool"],
+                           s["v_pool"], s["new_len"])
+        return {"k_pool": s["k_pool"], "v_pool": s["v_pool"], "new_len": s["new_len"]}
+    aj.aj_cache_attend(h, s["q"], s["k_pool"], s["v_pool"], s["table"], s["cache_len"], c["D"] ** -0.5, s["out"], lse=s["lse"],
+                       n_rows=s["n_rows"], depth=s["depth"], mask=s["mask"], k_scale=s["k_scale"], v_scale=s["v_scale"])
+    return {"out": s["out"], "lse": s["lse"]}
+
+
+def _run_plain(s):
+    c = s["case"]
+    return {"mask": _plain_mask, "append": _plain_append, "commit": _plain_commit, "attend": _plain_attend}[c["op"]](s, c)
+
+
+def _plain_mask(s, c):
+    reach = _reach(s["parent"])
+    s["depth"].copy_(reach.sum(2) - 1)
+    s["mask"].copy_(_pack(reach > 0.5))
+    return {"depth": s["depth"], "mask": s["mask"]}
+
+
+def _bits(pool):
+    """FP8 storage as bytes: indexing knows no FP8."""
+    return pool.view(torch.uint8) if pool.dtype == torch.float8_e4m3fn else pool
+
+
+def _take(pool, at):
+    """Rows of the pool, widened to 32 bits."""
+    return _bits(pool).flatten(0, 1)[at].view(pool.dtype).float()
+
+
+def _slots(s, c, t):
+    """Row of the pool (pages and slots in one axis) of token t of every window."""
+    page = c["page"]
+    return torch.gather(s["table"].long(), 1, t // page) * page + t % page
+
+
+def _live(s, c):
+    r = torch.arange(c["K"] + 1, device=DEVICE)
+    return r < (s["n_rows"][:, None] if s["n_rows"] is not None else c["K"] + 1), r
+
+
+def _plain_append(s, c):
+    B, K, D, nq, nkv, rot = c["B"], c["K"], c["D"], c["n_q"], c["n_kv"], c["rot"]
+    live, r = _live(s, c)
+    live = live.expand(B, K + 1)
+    depth = s["depth"] if s["depth"] is not None else r
+    angle = (s["cache_len"][:, None] + depth).double()[..., None] * s["inv_freq"].double()
+    cos, sin = angle.cos().float()[:, :, None], angle.sin().float()[:, :, None]
+
+    def norm(x, w):
+        x = x.unflatten(2, (-1, D)).float()
+        return x if w is None else x * (x.square().mean(-1, keepdim=True) + EPS).rsqrt() * w.float()
+
+    def turn(x):
+        if c.get("style") == "interleaved":
+            a, b = x[..., 0:rot:2], x[..., 1:rot:2]
+            y = torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2)
+        else:
+            a, b = x[..., : rot // 2], x[..., rot // 2 : rot]
+            y = torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+        return torch.cat([y, x[..., rot:]], -1)
+
+    q, k, v = turn(norm(s["q"], s["q_norm"])), turn(norm(s["k"], s["k_norm"])), s["v"].unflatten(2, (-1, D)).float()
+    s["q_out"].copy_(torch.where(live[..., None], q.flatten(2).to(s["q_out"].dtype), s["q_out"]))
+    at = _slots(s, c, s["cache_len"].long()[:, None] + r)
+    for pool, x, scale in ((s["k_pool"], k, s["k_scale"]), (s["v_pool"], v, s["v_scale"])):
+        x = (x / scale).clamp(-448, 448) if c["kv"] == "fp8" else x
+        x = torch.where(live[..., None, None], x, _take(pool, at)).to(pool.dtype)
+        _bits(pool).flatten(0, 1)[at] = _bits(x)
+    return {"q": s["q_out"], "k_pool": s["k_pool"], "v_pool": s["v_pool"]}
+
+
+def _plain_commit(s, c):
+    B, K = c["B"], c["K"]
+    reach = _reach(s["parent"])
+    rows = (s["out_node"].long() + 1).clamp(0, K)
+    on = reach[torch.arange(B, device=DEVICE), rows] > 0.5                # rows of the accepted path, the root's among them
+    n = on.sum(1)
+    r = torch.arange(K + 1, device=DEVICE)
+    source = torch.where(r < n[:, None], torch.where(on, r, r + K + 1).argsort(1), r)
+    first = s["cache_len"].long()[:, None]
+    to, of = _slots(s, c, first + r), _slots(s, c, first + source)
+    for pool in (s["k_pool"], s["v_pool"]):
+        flat = _bits(pool).flatten(1, 2)
+        flat[:, to] = flat[:, of]
+    s["new_len"].copy_(s["cache_len"] + n)
+    return {"k_pool": s["k_pool"], "v_pool": s["v_pool"], "new_len": s["new_len"]}
+
+
+def _plain_attend(s, c):
+    B, K, D, nq, nkv, w = c["B"], c["K"], c["D"], c["n_q"], c["n_kv"], c.get("window", 0)
+    R, G = K + 1, nq // nkv
+    live, r = _live(s, c)
+    T = c["hi"] + R
+    t = torch.arange(T, device=DEVICE)
+    first = s["cache_len"].long()[:, None]
+    at = _slots(s, c, t.expand(B, T).clamp(max=s["table"].shape[1] * c["page"] - 1)).clamp(min=0)
+    there = t < first + R
+    new = (t - first).clamp(0, K)                                         # row of a new token
+    seen = (t < first)[:, None] | (there & (t >= first))[:, None] & (new[:, None] <= r[:, None])
+    pos_r, pos_t = first + r, torch.where(t < first, t, first + new)
+    if s["mask"] is not None:
+        word = torch.gather(s["mask"], 2, (new // 32)[:, None].expand(B, R, T))
+        seen &= (t < first)[:, None] | ((word >> (new % 32)[:, None].int()) & 1).bool()
+        pos_r, pos_t = first + s["depth"], torch.where(t < first, t, first + torch.gather(s["depth"].long(), 1, new))
+    if w:
+        seen &= (pos_r[:, :, None] - pos_t[:, None] < w) | (pos_t < SINKS)[:, None]
+    k = _take(s["k_pool"], at) * s["k_scale"]              # [B, T, n_kv, D]
+    v = torch.where(there[..., None, None], _take(s["v_pool"], at) * s["v_scale"], 0.0)
+    q = s["q"].float().view(B, R, nkv, G, D).permute(0, 2, 3, 1, 4).reshape(B, nkv, G * R, D)
+    x = (q @ k.permute(0, 2, 3, 1).contiguous()).mul_(D ** -0.5).view(B, nkv, G, R, T)
+    del k
+    x.masked_fill_(~seen[:, None, None], -math.inf)
+    m = x.amax(-1, keepdim=True)
+    base = torch.where(m == -math.inf, 0.0, m)
+    x = x.sub_(base).exp_()
+    total = x.sum(-1, keepdim=True)
+    out = (x.view(B, nkv, G * R, T) @ v.permute(0, 2, 1, 3).contiguous()).view(B, nkv, G, R, D)
+    out = torch.where(total > 0, out / total, 0.0).permute(0, 3, 1, 2, 4).reshape(B, R, nq * D)
+    lse = (base + total.log()).squeeze(-1).permute(0, 3, 1, 2).reshape(B, R, nq)
+    live = live.expand(B, R)[..., None]
+    s["out"].copy_(torch.where(live, out.to(s["out"].dtype), s["out"]))
+    s["lse"].copy_(torch.where(live, lse, s["lse"]))
+    return {"out": s["out"], "lse": s["lse"]}
+
+
+# --- the definition, window by window, in 64 bits -------------------------------------------------------------------
+
+def exact(c, seed):
+    if c["op"] == "mask":
+        return None                                                       # whole numbers
+    global own
+    before, own = own, False
+    try:
+        s = prepare(c, seed)
+    finally:
+        own = before
+    return {"append": _exact_append, "attend": _exact_attend, "commit": _exact_commit}[c["op"]](s, c)
+
+
+def _rows_of(table, page, t):
+    return table[t // page].long() * page + t % page
+
+
+def _exact_append(s, c):
+    D, rot, page = c["D"], c["rot"], c["page"]
+    lens, rows = _lengths(c)
+    q_out, pools = s["q_out"].double(), [s["k_pool"].double(), s["v_pool"].double()]
+
+    def one(x, w, pos):
+        x = x.double().reshape(x.shape[0], x.shape[1] // D, D)
+        if w is not None:
+            x = x / torch.sqrt((x * x).sum(-1, keepdim=True) / D + EPS) * w.double()
+        if rot:
+            even = torch.arange(0, rot, 2, device=x.device) if c.get("style") == "interleaved" else torch.arange(rot // 2, device=x.device)
+            odd = even + (1 if c.get("style") == "interleaved" else rot // 2)
+            z = torch.complex(x[..., even], x[..., odd])
+            z = z * torch.polar(torch.ones((), dtype=torch.float64, device=x.device), pos[:, None] * s["inv_freq"].double())[:, None]
+            x[..., even], x[..., odd] = z.real, z.imag
+        return x
+
+    for b, (L, n) in enumerate(zip(lens, rows)):
+        pos = L + (s["depth"][b, :n].double() if s["depth"] is not None else torch.arange(n, device=DEVICE).double())
+        q_out[b, :n] = one(s["q"][b, :n], s["q_norm"], pos).flatten(1)
+        at = _rows_of(s["table"][b], page, L + torch.arange(n, device=DEVICE))
+        pools[0].view(-1, c["n_kv"], D)[at] = one(s["k"][b, :n], s["k_norm"], pos) / s["k_scale"]
+        pools[1].view(-1, c["n_kv"], D)[at] = s["v"][b, :n].double().reshape(n, c["n_kv"], D) / s["v_scale"]
+    if c["kv"] == "fp8":
+        pools = [p.clamp(-448, 448) for p in pools]
+    return {"q": q_out, "k_pool": pools[0], "v_pool": pools[1]}
+
+
+def _exact_attend(s, c):
+    D, nq, nkv, page, w = c["D"], c["n_q"], c["n_kv"], c["page"], c.get("window", 0)
+    lens, rows = _lengths(c)
+    out, lse = s["out"].double(), s["lse"].double()
+    keys, values = (_bits(s[p]).view(-1, nkv, D) for p in ("k_pool", "v_pool"))
+    wide = lambda x: x.view(s["k_pool"].dtype).double()  # noqa: E731
+    for b, (L, n) in enumerate(zip(lens, rows)):
+        if not n:
+            continue
+        at = _rows_of(s["table"][b], page, torch.arange(L + n, device=DEVICE))
+        depth = torch.arange(n, device=DEVICE)
+        edge = torch.ones(n, n, device=DEVICE).tril().bool()
+        if s["mask"] is not None:
+            depth = s["depth"][b, :n].long()
+            bits = (s["mask"][b, :n, :, None] >> torch.arange(32, device=DEVICE, dtype=torch.int32)) & 1
+            edge &= bits.flatten(1)[:, :n].bool()
+        seen = torch.cat([torch.ones(n, L, dtype=torch.bool, device=DEVICE), edge], 1)
+        if w:
+            pos = torch.cat([torch.arange(L, device=DEVICE), L + depth])
+            seen &= ((L + depth)[:, None] - pos < w) | (pos < SINKS)
+        q = s["q"][b, :n].double().view(n, nkv, nq // nkv, D)
+        for h in range(nkv):
+            k, v = wide(keys[at, h]) * s["k_scale"], wide(values[at, h]) * s["v_scale"]
+            x = (q[:, h] @ k.T) / math.sqrt(D)
+            x = torch.where(seen[:, None], x, -math.inf)
+            lse[b, :n].view(n, nkv, -1)[:, h] = torch.logsumexp(x, -1)
+            out[b, :n].view(n, nkv, -1, D)[:, h] = torch.softmax(x, -1) @ v
+    return {"out": out, "lse": lse}
+
+
+def _exact_commit(s, c):
+    page = c["page"]
+    lens, _ = _lengths(c)
+    parent, node, table = s["parent"].tolist(), s["out_node"].tolist(), s["table"].tolist()
+    pools = [s["k_pool"].double().flatten(1, 2), s["v_pool"].double().flatten(1, 2)]
+    new = []
+    for b, L in enumerate(lens):
+        path, j = [], node[b]
+        while j >= 0:
+            path.append(j)
+            j = parent[b][j]
+        path.reverse()
+        slot = lambda t: table[b][t // page] * page + t % page  # noqa: E731
+        to = torch.tensor([slot(L + 1 + i) for i in range(len(path))], dtype=torch.long, device=DEVICE)
+        of = torch.tensor([slot(L + 1 + j) for j in path], dtype=torch.long, device=DEVICE)
+        for p in pools:
+            p[:, to] = p[:, of]
+        new.append(L + 1 + len(path))
+    return {"k_pool": pools[0].view_as(s["k_pool"]), "v_pool": pools[1].view_as(s["v_pool"]), "new_len": torch.tensor(new, dtype=torch.int32, device=DEVICE)}
