@@ -83,7 +83,7 @@ def draw(rng):
                 hi, lo = (hi + 1) // 2, (lo + 1) // 2
             c = _case("", op, B, K, n_q, n_kv, D, dtype, kv, page, lo, hi, **more)
     elif op == "mask":
-        K = max(1, K) if rng.random() < 0.5 else int(_log_uniform(rng, 8, 501))
+        K = max(8, K) if rng.random() < 0.5 else int(_log_uniform(rng, 8, 501))
         n_q, n_kv, D, dtype, kv, page, lo, hi = 32, 8, 128, "bf16", "same", 16, 0, 256
     else:
         K = max(1, min(K, 64))
@@ -141,7 +141,7 @@ def _trees(c, g):
 
 
 def _reach(parent):
-    """[B, K+1, K+1] of 0 and 1: row r has a 1 at itself and at its ancestors (row 0 is the root, row j+1 is node j)."""
+    """[B, K+1, K+1] of 0.0 and 1.0: row r has a 1 at itself and at its ancestors (row 0 is the root, row j+1 is node j)."""
     B, K = parent.shape
     up = torch.zeros(B, K + 1, K + 1, device=parent.device)
     up.scatter_(2, torch.nn.functional.pad(parent.long() + 1, (1, 0))[:, :, None], 1.0)
@@ -218,7 +218,7 @@ def prepare(c, seed):
         del x
     s["k_pool"], s["v_pool"] = pools
     s["depth"] = s["mask"] = None
-    if c.get("tree"):
+    if c.get("tree") or c["op"] == "commit":
         reach = _reach(s["parent"])
         s["depth"] = (reach.sum(2) - 1).to(torch.int32).contiguous()
         s["mask"] = _pack(reach > 0.5).contiguous()
@@ -267,7 +267,7 @@ def _run_own(s):
                            s["k_pool"], s["v_pool"], n_rows=s["n_rows"], depth=s["depth"], k_scale=s["k_scale"], v_scale=s["v_scale"])
         return {"q": s["q_out"], "k_pool": s["k_pool"], "v_pool": s["v_pool"]}
     if c["op"] == "commit":
-        aj.aj_cache_commit(h, s["parent"], s["out_node"], s["table"], s["cache_len"], c["layers"], s["k_pool"].stride(0), s["k_pool"],
+        aj.aj_cache_commit(h, s["mask"], s["out_node"], s["table"], s["cache_len"], c["layers"], s["k_pool"].stride(0), s["k_pool"],
                            s["v_pool"], s["new_len"])
         return {"k_pool": s["k_pool"], "v_pool": s["v_pool"], "new_len": s["new_len"]}
     aj.aj_cache_attend(h, s["q"], s["k_pool"], s["v_pool"], s["table"], s["cache_len"], c["D"] ** -0.5, s["out"], lse=s["lse"],
@@ -341,11 +341,10 @@ def _plain_append(s, c):
 
 def _plain_commit(s, c):
     B, K = c["B"], c["K"]
-    reach = _reach(s["parent"])
-    rows = (s["out_node"].long() + 1).clamp(0, K)
-    on = reach[torch.arange(B, device=DEVICE), rows] > 0.5                # rows of the accepted path, the root's among them
-    n = on.sum(1)
     r = torch.arange(K + 1, device=DEVICE)
+    words = s["mask"][torch.arange(B, device=DEVICE), (s["out_node"].long() + 1).clamp(0, K)]
+    on = (words[:, r // 32] >> (r % 32).int()) & 1 > 0                    # rows of the accepted path, the root's among them
+    n = on.sum(1)
     source = torch.where(r < n[:, None], torch.where(on, r, r + K + 1).argsort(1), r)
     first = s["cache_len"].long()[:, None]
     to, of = _slots(s, c, first + r), _slots(s, c, first + source)
