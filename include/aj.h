@@ -263,6 +263,107 @@ int aj_debug_tile(const aj_handle *h, int32_t *vocab_rows, int32_t *verify_rows)
  */
 int aj_debug_form(const aj_handle *h, int32_t *waves, int32_t *vocab_blocks, int32_t *k_order);
 
+/* ---- Around the verification step: the target's paged cache of keys and values --------------------------------------
+ *
+ * What a server runs in every layer on the same windows before aj_verify*, and once after it: the new rows of B windows of
+ * K+1 rows each go into the cache (aj_cache_append), attend over it (aj_cache_attend), and after aj_verify_tree the accepted
+ * path is kept (aj_cache_commit).  K = 0 is plain decoding of one token per window.  Sections 2 and 3.3 of the paper leave this to the
+ * serving engine; these entry points serve its windows, chains and trees as aj_verify and aj_verify_tree read them.
+ *
+ * Tokens of a window b: t < L = cache_len[b] are cached, t = L + r is new row r (0 .. n_rows[b]-1).  Token t lives in page
+ * page_table[b][t / page_size], slot t % page_size.  Its position is t for cached tokens and L + depth[b][r] for new row r.
+ *
+ *   k_pool, v_pool   [n_pages][page_size][n_kv][head_dim]   (other orders by the strides of the configuration)
+ *   page_table [B][table_width] int32
+ *   cache_len  [B] int32      read as 0 where negative
+ *   n_rows     [B] int32      rows of a window that are there, clamped into [0, K+1]; NULL: K+1.  Rows behind them are not read, and what
+ *                             belongs to them in q_out, out, lse and the pools is left as it was
+ *   depth      [B][K+1] int32 position of row r behind L, clamped into [0, r]; NULL: r (a chain)
+ *   mask       [B][K+1][(K+32)/32] uint32   bit j % 32 of word j / 32: row r sees new row j; bits j > r count for nothing.  NULL: row r
+ *                             sees rows 0 .. r.  aj_tree_mask makes depth and mask from the parents of aj_verify_tree
+ * A token whose page number is outside [0, n_pages), or that lies behind the table (t >= table_width * page_size), is nowhere: it is
+ * not stored, and nothing sees it.  Slots that hold no visible token may hold anything, NaN included.  Pages may be shared by
+ * windows for reading; a slot that a call writes belongs to one window.
+ */
+typedef struct aj_cache aj_cache; /* opaque */
+
+enum { AJ_KV_SAME = 0, AJ_KV_FP8_E4M3 = 1 };
+enum { AJ_ROPE_HALF = 0, AJ_ROPE_INTERLEAVED = 1 };
+
+typedef struct {
+    int32_t B, K;         /* windows >= 0, draft tokens per window 0 <= K <= 1023; B * (K+1) < 2^24 */
+    int32_t n_q, n_kv;    /* heads of queries (a multiple of n_kv, at most 65535) and of keys and values; query head h reads head h / (n_q / n_kv) */
+    int32_t head_dim;     /* multiple of 16, 16 .. 256 */
+    int32_t dtype;        /* aj_dtype of q, k, v, q_norm, k_norm, q_out, out */
+    int32_t kv_dtype;     /* storage of the pools: AJ_KV_SAME (0) = `dtype`; AJ_KV_FP8_E4M3 = OCP FP8 E4M3 bytes, needs dtype = AJ_BF16 */
+    int32_t page_size;    /* tokens in a page: a power of two, 1 .. 65536 */
+    int32_t n_pages;      /* pages of the pools, >= 1 */
+    int32_t table_width;  /* page numbers of a window, >= 1; table_width * page_size < 2^31 */
+    int32_t window;       /* 0: every earlier token is visible.  w > 0: those at positions above p - w from position p, and ... */
+    int32_t sinks;        /* ... the tokens at positions below `sinks` (>= 0; must be 0 when window is 0) */
+    int32_t rot_dim;      /* elements of a head that are rotated: a multiple of 16 up to head_dim; 0: none */
+    int32_t rope;         /* AJ_ROPE_HALF: element i pairs with i + rot_dim/2; AJ_ROPE_INTERLEAVED: 2i with 2i + 1 */
+    int64_t page_stride, slot_stride, head_stride; /* of the pools, in elements; all three 0: as above.  Multiples of 16 bytes, > 0, and no two
+                             tokens' heads may overlap */
+    int64_t qkv_stride;   /* elements between rows of q, k and v of aj_cache_append (a fused projection); 0: n_q * head_dim and n_kv * head_dim */
+    int64_t q_stride;     /* elements between rows of q_out and of aj_cache_attend's q; 0: n_q * head_dim */
+    int32_t flags;        /* 0 */
+} aj_cache_config;
+
+/* Validate cfg, allocate the workspace of aj_cache_attend on the current device.  *out is NULL on failure.  A handle does not own the pools:
+   one handle serves all layers of a model.  As with aj_handle, one call in flight per handle. */
+int aj_cache_create(const aj_cache_config *cfg, aj_cache **out);
+
+/* Frees the workspace.  The caller must have synchronised any stream still using the handle. */
+int aj_cache_destroy(aj_cache *c);
+
+/*
+ * New rows into the cache, with the norms of queries and keys and the rotation of positions in the same pass.  Per head x of head_dim elements:
+ *     x = x * rsqrt(mean(x^2) + eps) * norm                                       (norm NULL: left out)
+ *     (x[i], x[i']) = (x[i] cos a - x[i'] sin a, x[i'] cos a + x[i] sin a)        for the rot_dim/2 pairs (i, i'), a = position * inv_freq[i]
+ * q -> q_out, k -> k_pool and, unchanged, v -> v_pool at the new rows' tokens; FP8 pools hold x / k_scale and x / v_scale, rounded to
+ * nearest even, values beyond +-448 as +-448.  Sums in fp32, angles in fp64; rounded once.
+ *   q [B][K+1][n_q][head_dim], k, v [B][K+1][n_kv][head_dim]     rows qkv_stride apart; may be parts of one tensor
+ *   q_norm, k_norm [head_dim] or NULL;  inv_freq [rot_dim/2] float (NULL when rot_dim is 0)
+ *   q_out [B][K+1][n_q][head_dim], rows q_stride apart; may be q itself when their strides agree
+ * AJ_EINVAL on null / misaligned pointers, eps < 0 or not finite, scales that are not positive and finite (FP8 pools) or not 1 (others); AJ_ESTATE
+ * when the current device is not the handle's; AJ_EHIP on a launch failure.
+ */
+int aj_cache_append(aj_cache *c, const void *q, const void *k, const void *v, const void *q_norm, const void *k_norm, float eps,
+                    const float *inv_freq, const int32_t *page_table, const int32_t *cache_len, const int32_t *n_rows, const int32_t *depth,
+                    float k_scale, float v_scale, void *q_out, void *k_pool, void *v_pool, void *stream);
+
+/*
+ * Attention of the new rows over the cache, which holds the new rows themselves already (aj_cache_append):
+ *     s[t] = scale * q . (k_scale * k_pool[t]),  out = sum_t softmax(s)[t] * (v_scale * v_pool[t]),  lse = log sum_t exp(s[t])
+ * over the tokens t that row r sees: cached tokens, and new rows by `mask` or up to itself; of these, with a window, those at positions above
+ * position(r) - window or below sinks.  A row that sees nothing gives out = 0 and lse = -inf.
+ *   q   [B][K+1][n_q][head_dim]   rows q_stride apart
+ *   out [B][K+1][n_q][head_dim]   dense;   lse [B][K+1][n_q] float or NULL
+ * Scores, their maxima and sums and the weighted sums are held in fp32; with bf16 the weights are rounded to bf16 before they meet the
+ * values.  The same call gives the same bits.  Errors as aj_cache_append, and AJ_EINVAL unless scale * k_scale is positive and finite.
+ */
+int aj_cache_attend(aj_cache *c, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table, const int32_t *cache_len,
+                    const int32_t *n_rows, const int32_t *depth, const uint32_t *mask, float scale, float k_scale, float v_scale,
+                    void *out, float *lse, void *stream);
+
+/*
+ * Depths and masks of draft trees: row 0 is the root, row j + 1 is node j.  parent [B][K] as in aj_verify_tree (values outside [-1, j)
+ * are clamped into it).  depth [B][K+1]: ancestors of a row; mask [B][K+1][(K+32)/32]: bit i of row r is set when row i is row r or an
+ * ancestor of it.  Once per step serves all layers.  1 <= K <= 1023, B >= 0.
+ */
+int aj_tree_mask(int32_t B, int32_t K, const int32_t *parent, int32_t *depth, uint32_t *mask, void *stream);
+
+/*
+ * After aj_verify_tree: the rows on the way from the root to out_node[b] (clamped into [-1, K); bits j <= out_node + 1 of that node's mask
+ * row, the root's always) move to the tokens L, L + 1, ... of window b in ascending order, in the pools of n_layers layers that lie
+ * layer_stride elements apart.  new_len [B] = L + the number of these rows.  All other slots keep what they hold.  (After aj_verify nothing has
+ * to move: the new length is L + 1 + out_len.)  A row that moves from or to a token that is nowhere is skipped.  new_len may not be
+ * cache_len.  n_layers >= 0; layer_stride a positive multiple of 16 bytes (any value for one layer).  Errors as aj_cache_append.
+ */
+int aj_cache_commit(aj_cache *c, const uint32_t *mask, const int32_t *out_node, const int32_t *page_table, const int32_t *cache_len,
+                    int32_t n_layers, int64_t layer_stride, void *k_pool, void *v_pool, int32_t *new_len, void *stream);
+
 const char *aj_strerror(int status);
 int aj_last_hip_error(void); /* hipError_t of the last AJ_EHIP on this thread */
 

@@ -18,10 +18,13 @@ _LIB_PATH = os.environ.get("AJ_LIBRARY") or os.path.join(_HERE, "libaj.so")
 AJ_F32, AJ_BF16 = 0, 1
 AJ_FLAG_DEBUG, AJ_FLAG_PROFILE, AJ_FLAG_TOPK, AJ_FLAG_FUSED_JUDGE = 1, 2, 4, 8
 AJ_W_SAME, AJ_W_FP8_E4M3 = 0, 1
+AJ_KV_SAME, AJ_KV_FP8_E4M3 = 0, 1
+AJ_ROPE_HALF, AJ_ROPE_INTERLEAVED = 0, 1
 AJ_KERNEL_AUTO, AJ_KERNEL_TILE, AJ_KERNEL_STREAM, AJ_KERNEL_BIG, AJ_KERNEL_TALL, AJ_KERNEL_PAIR, AJ_KERNEL_PAIR9, AJ_KERNEL_RESIDENT, AJ_KERNEL_WIDE = 0, 1, 2, 3, 4, 5, 6, 7, 8
 
 SYMBOLS = ["aj_create", "aj_verify", "aj_verify_static", "aj_verify_sampled", "aj_verify_tree", "aj_verify_topk", "aj_debug_copy_rank", "aj_destroy", "aj_debug_ptrs", "aj_debug_copy", "aj_debug_logits",
-           "aj_profile_read", "aj_kernel_name", "aj_debug_tile", "aj_debug_form", "aj_strerror", "aj_last_hip_error"]
+           "aj_profile_read", "aj_kernel_name", "aj_debug_tile", "aj_debug_form", "aj_strerror", "aj_last_hip_error",
+           "aj_cache_create", "aj_cache_destroy", "aj_cache_append", "aj_cache_attend", "aj_cache_commit", "aj_tree_mask"]
 
 
 class AjError(RuntimeError):
@@ -33,6 +36,13 @@ class AjError(RuntimeError):
 class _Config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("B", "K", "d_t", "d_d", "V", "dtype", "feat_offset", "flags", "kernel", "w_dtype")]
+
+
+class _CacheConfig(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in
+                 ("B", "K", "n_q", "n_kv", "head_dim", "dtype", "kv_dtype", "page_size", "n_pages", "table_width", "window", "sinks", "rot_dim",
+                  "rope")] + [(n, ctypes.c_int64) for n in ("page_stride", "slot_stride", "head_stride", "qkv_stride", "q_stride")]
+                + [("flags", ctypes.c_int32)])
 
 
 _lib = None
@@ -85,6 +95,18 @@ def load_library():
     lib.aj_debug_tile.restype = ctypes.c_int
     lib.aj_debug_form.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32)]
     lib.aj_debug_form.restype = ctypes.c_int
+    lib.aj_cache_create.argtypes = [ctypes.POINTER(_CacheConfig), ctypes.POINTER(vp)]
+    lib.aj_cache_create.restype = ctypes.c_int
+    lib.aj_cache_destroy.argtypes = [vp]
+    lib.aj_cache_destroy.restype = ctypes.c_int
+    lib.aj_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp, f32, f32, vp, vp, vp, vp]
+    lib.aj_cache_append.restype = ctypes.c_int
+    lib.aj_cache_attend.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, f32, f32, f32, vp, vp, vp]
+    lib.aj_cache_attend.restype = ctypes.c_int
+    lib.aj_cache_commit.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.c_int64, vp, vp, vp, vp]
+    lib.aj_cache_commit.restype = ctypes.c_int
+    lib.aj_tree_mask.argtypes = [i32, i32, vp, vp, vp, vp]
+    lib.aj_tree_mask.restype = ctypes.c_int
     lib.aj_strerror.argtypes = [ctypes.c_int]
     lib.aj_strerror.restype = ctypes.c_char_p
     lib.aj_last_hip_error.argtypes = []
@@ -112,6 +134,15 @@ def _ptr(t):
         raise ValueError("libaj takes device tensors")
     if not t.is_contiguous():
         raise ValueError("libaj takes contiguous row-major tensors")
+    return t.data_ptr()
+
+
+def _ptr_strided(t):
+    """As _ptr, for what the configuration gives strides of (pools, rows of queries, keys and values)."""
+    if t is None or isinstance(t, int):
+        return t
+    if not t.is_cuda:
+        raise ValueError("libaj takes device tensors")
     return t.data_ptr()
 
 
@@ -252,6 +283,58 @@ def aj_profile_read(h, capacity=64):
     if rc != 0:
         raise AjError(rc, "aj_profile_read")
     return [float(ms[i]) for i in range(n.value)]
+
+
+def aj_cache_create(B, K, n_q, n_kv, head_dim, page_size, n_pages, table_width, dtype=AJ_BF16, kv_dtype=AJ_KV_SAME, window=0, sinks=0,
+                    rot_dim=0, rope=AJ_ROPE_HALF, page_stride=0, slot_stride=0, head_stride=0, qkv_stride=0, q_stride=0, flags=0):
+    """A handle for the paged cache's calls.  Strides in elements; 0: dense."""
+    cfg = _CacheConfig(B, K, n_q, n_kv, head_dim, dtype, kv_dtype, page_size, n_pages, table_width, window, sinks, rot_dim, rope, page_stride,
+                       slot_stride, head_stride, qkv_stride, q_stride, flags)
+    h = ctypes.c_void_p()
+    rc = load_library().aj_cache_create(ctypes.byref(cfg), ctypes.byref(h))
+    if rc != 0:
+        raise AjError(rc, "aj_cache_create")
+    return h
+
+
+def aj_cache_destroy(h):
+    rc = load_library().aj_cache_destroy(h)
+    if rc != 0:
+        raise AjError(rc, "aj_cache_destroy")
+
+
+def aj_cache_append(h, q, k, v, q_norm, k_norm, eps, inv_freq, page_table, cache_len, q_out, k_pool, v_pool, n_rows=None, depth=None, k_scale=1.0,
+                    v_scale=1.0, stream=None):
+    """New rows' queries, keys and values: norms, rotation, keys and values into the pools."""
+    rc = load_library().aj_cache_append(h, _ptr_strided(q), _ptr_strided(k), _ptr_strided(v), _ptr(q_norm), _ptr(k_norm), float(eps), _ptr(inv_freq),
+                                        _ptr(page_table), _ptr(cache_len), _ptr(n_rows), _ptr(depth), float(k_scale), float(v_scale),
+                                        _ptr_strided(q_out), _ptr_strided(k_pool), _ptr_strided(v_pool), _stream(stream))
+    if rc != 0:
+        raise AjError(rc, "aj_cache_append")
+
+
+def aj_cache_attend(h, q, k_pool, v_pool, page_table, cache_len, scale, out, lse=None, n_rows=None, depth=None, mask=None, k_scale=1.0, v_scale=1.0,
+                    stream=None):
+    """Attention of the new rows over the cache; mask (the bits as int32 or uint32) and depth from aj_tree_mask for trees."""
+    rc = load_library().aj_cache_attend(h, _ptr_strided(q), _ptr_strided(k_pool), _ptr_strided(v_pool), _ptr(page_table), _ptr(cache_len), _ptr(n_rows),
+                                        _ptr(depth), _ptr(mask), float(scale), float(k_scale), float(v_scale), _ptr(out), _ptr(lse), _stream(stream))
+    if rc != 0:
+        raise AjError(rc, "aj_cache_attend")
+
+
+def aj_tree_mask(B, K, parent, depth, mask, stream=None):
+    """Depths [B, K+1] and masks [B, K+1, (K+32)//32] of draft trees."""
+    rc = load_library().aj_tree_mask(B, K, _ptr(parent), _ptr(depth), _ptr(mask), _stream(stream))
+    if rc != 0:
+        raise AjError(rc, "aj_tree_mask")
+
+
+def aj_cache_commit(h, mask, out_node, page_table, cache_len, n_layers, layer_stride, k_pool, v_pool, new_len, stream=None):
+    """The accepted path's rows to the front of their windows' new tokens, in all layers; new_len [B] the new lengths."""
+    rc = load_library().aj_cache_commit(h, _ptr(mask), _ptr(out_node), _ptr(page_table), _ptr(cache_len), int(n_layers), int(layer_stride),
+                                        _ptr_strided(k_pool), _ptr_strided(v_pool), _ptr(new_len), _stream(stream))
+    if rc != 0:
+        raise AjError(rc, "aj_cache_commit")
 
 
 def device_tensor(a: np.ndarray, device="cuda:0"):

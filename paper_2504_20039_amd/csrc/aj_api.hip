@@ -41,7 +41,7 @@ struct aj_handle {
 
 static thread_local int g_last_hip = 0;
 
-static int hip_fail(hipError_t e)
+int aj::hip_fail(hipError_t e)
 {
     g_last_hip = (int)e;
     return AJ_EHIP;

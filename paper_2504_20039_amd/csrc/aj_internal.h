@@ -10,6 +10,9 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
+// keeps e for aj_last_hip_error on this thread; returns AJ_EHIP
+int hip_fail(hipError_t e);
+
 // (value, index) pair ordered by larger value, then lower index.
 struct __attribute__((aligned(8))) Best {
     float v;
