@@ -291,14 +291,15 @@ enum { AJ_KV_SAME = 0, AJ_KV_FP8_E4M3 = 1 };
 enum { AJ_ROPE_HALF = 0, AJ_ROPE_INTERLEAVED = 1 };
 
 typedef struct {
-    int32_t B, K;         /* windows >= 0, draft tokens per window 0 <= K <= 1023; B * (K+1) < 2^24 */
-    int32_t n_q, n_kv;    /* heads of queries (a multiple of n_kv, at most 65535) and of keys and values; query head h reads head h / (n_q / n_kv) */
+    int32_t B, K;         /* windows >= 0, draft tokens per window 0 <= K <= 1023; B * (K+1) < 2^24; B * n_kv * (table_width *
+                             page_size / 32 + 2) <= 2 10^9 */
+    int32_t n_q, n_kv;    /* heads of queries (a multiple of n_kv, at most 1024) and of keys and values; query head h reads head h / (n_q / n_kv) */
     int32_t head_dim;     /* multiple of 16, 16 .. 256 */
     int32_t dtype;        /* aj_dtype of q, k, v, q_norm, k_norm, q_out, out */
     int32_t kv_dtype;     /* storage of the pools: AJ_KV_SAME (0) = `dtype`; AJ_KV_FP8_E4M3 = OCP FP8 E4M3 bytes, needs dtype = AJ_BF16 */
     int32_t page_size;    /* tokens in a page: a power of two, 1 .. 65536 */
     int32_t n_pages;      /* pages of the pools, >= 1 */
-    int32_t table_width;  /* page numbers of a window, >= 1; table_width * page_size < 2^31 */
+    int32_t table_width;  /* page numbers of a window, >= 1; table_width * page_size <= 2^30 */
     int32_t window;       /* 0: every earlier token is visible.  w > 0: those at positions above p - w from position p, and ... */
     int32_t sinks;        /* ... the tokens at positions below `sinks` (>= 0; must be 0 when window is 0) */
     int32_t rot_dim;      /* elements of a head that are rotated: a multiple of 16 up to head_dim; 0: none */

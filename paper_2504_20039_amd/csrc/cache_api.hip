@@ -14,6 +14,9 @@ struct aj_cache {
     int es, kv_es;         // bytes of an element of q, k, v, out; of the pools
     int log_page;
     int device;
+    AttendPlan plan;
+    float *part_o;         // partial results of aj_cache_attend
+    float2 *part_ml;
 };
 
 static bool aligned(const void *p, unsigned n) { return (((uintptr_t)p) & (n - 1)) == 0; }
@@ -23,12 +26,12 @@ static bool plan_cache(const aj_cache_config &cfg, aj_cache *h)
     h->cfg = cfg;
     aj_cache_config &c = h->cfg;
     if (c.B < 0 || c.K < 0 || c.K > 1023 || (int64_t)c.B * (c.K + 1) >= (1 << 24)) return false;
-    if (c.n_kv < 1 || c.n_q < 1 || c.n_q > 65535 || c.n_q % c.n_kv) return false;
+    if (c.n_kv < 1 || c.n_q < 1 || c.n_q > 1024 || c.n_q % c.n_kv) return false;
     if (c.head_dim < 16 || c.head_dim > 256 || c.head_dim % 16) return false;
     if (c.dtype != AJ_F32 && c.dtype != AJ_BF16) return false;
     if (c.kv_dtype != AJ_KV_SAME && !(c.kv_dtype == AJ_KV_FP8_E4M3 && c.dtype == AJ_BF16)) return false;
     if (c.page_size < 1 || c.page_size > 65536 || (c.page_size & (c.page_size - 1))) return false;
-    if (c.n_pages < 1 || c.table_width < 1 || (int64_t)c.table_width * c.page_size >= (1LL << 31)) return false;
+    if (c.n_pages < 1 || c.table_width < 1 || (int64_t)c.table_width * c.page_size > (1 << 30)) return false;
     if (c.window < 0 || c.sinks < 0 || (c.window == 0 && c.sinks)) return false;
     if (c.rot_dim < 0 || c.rot_dim > c.head_dim || c.rot_dim % 16) return false;
     if (c.rope != AJ_ROPE_HALF && c.rope != AJ_ROPE_INTERLEAVED) return false;
@@ -53,6 +56,13 @@ static bool plan_cache(const aj_cache_config &cfg, aj_cache *h)
     return true;
 }
 
+static void free_cache(aj_cache *h)
+{
+    if (h->part_o) (void)hipFree(h->part_o);
+    if (h->part_ml) (void)hipFree(h->part_ml);
+    delete h;
+}
+
 extern "C" int aj_cache_create(const aj_cache_config *cfg, aj_cache **out)
 {
     if (out) *out = nullptr;
@@ -63,10 +73,30 @@ extern "C" int aj_cache_create(const aj_cache_config *cfg, aj_cache **out)
         delete h;
         return AJ_EINVAL;
     }
-    const hipError_t e = hipGetDevice(&h->device);
+    const aj_cache_config &c = h->cfg;
+    // places of the line of tiles are counted in 32 bits (tiles have 32 tokens or more)
+    if ((double)c.B * c.n_kv * ((double)c.table_width * c.page_size / 32 + 2) > 2e9) {
+        delete h;
+        return AJ_EINVAL;
+    }
+    int cus = 0;
+    hipError_t e = hipGetDevice(&h->device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, h->device);
     if (e != hipSuccess) {
         delete h;
         return hip_fail(e);
+    }
+    if (c.B > 0) {
+        const int vectors = (c.K + 1) * (c.n_q / c.n_kv);
+        h->plan = h->type == CACHE_F32   ? cache_attend_plan_f32(c.head_dim, vectors, cus)
+                  : h->type == CACHE_FP8 ? cache_attend_plan_fp8(c.head_dim, vectors, cus)
+                                         : cache_attend_plan_bf16(c.head_dim, vectors, cus);
+        const size_t units = (size_t)h->plan.clusters * 2 * h->plan.blocks * h->plan.vectors;
+        if (hipMalloc(&h->part_o, h->plan.part_floats * sizeof(float)) != hipSuccess || hipMalloc(&h->part_ml, units * sizeof(float2)) != hipSuccess) {
+            (void)hipGetLastError();
+            free_cache(h);
+            return AJ_ENOMEM;
+        }
     }
     *out = h;
     return AJ_OK;
@@ -75,7 +105,7 @@ extern "C" int aj_cache_create(const aj_cache_config *cfg, aj_cache **out)
 extern "C" int aj_cache_destroy(aj_cache *h)
 {
     if (!h) return AJ_EINVAL;
-    delete h;
+    free_cache(h);
     return AJ_OK;
 }
 
@@ -188,7 +218,13 @@ extern "C" int aj_cache_attend(aj_cache *h, const void *q, const void *k_pool, c
     a.q_stride = c.q_stride;
     a.score_scale = score_scale;
     a.v_scale = v_scale;
-    const hipError_t e = cache_attend(h->type, a, (hipStream_t)stream);
+    a.clusters = h->plan.clusters;
+    a.blocks = h->plan.blocks;
+    a.part_o = h->part_o;
+    a.part_ml = h->part_ml;
+    const bool few = (c.K + 1) * (c.n_q / c.n_kv) <= 32;
+    hipStream_t s = (hipStream_t)stream;
+    const hipError_t e = h->type == CACHE_F32 ? cache_attend_f32(few, a, s) : h->type == CACHE_FP8 ? cache_attend_fp8(few, a, s) : cache_attend_bf16(few, a, s);
     return e == hipSuccess ? AJ_OK : hip_fail(e);
 }
 

@@ -1,0 +1,663 @@
+// Attention of the new rows of speculation windows over the paged cache (aj_cache_attend).
+//
+// A window's R rows and the G query heads that share a head of keys and values are R*G query vectors against the same tokens: vector x = r * G + g.
+// A workgroup takes up to QB of them and walks over tiles of ST tokens with the running maximum and sum of a softmax; scores and weights
+// never leave its registers.
+//
+// Products.  v_mfma 32x32: scores S^T = K Q^T (A = 32 tokens, B = 32 vectors), so that a lane owns one vector and 16 of 32 tokens: maximum and sum run in
+// the lane, with one exchange between the wave's halves.  Then O^T = V^T P^T: the weights are needed as the B operand, where lane (column, half h) holds
+// 8 consecutive places of the contraction; which token stands at which place is free as long as V^T agrees, so the weights stay where the scores were
+// made (a half's registers 8s .. 8s+7 are tokens 16s + 4h + {0..3} and 16s + 8 + 4h + {0..3}) and V^T's fragments are gathered in that order: bf16 and
+// FP8 by the transposing LDS reads (ds_read_b64_tr_b16 / _b8: 16 lanes read 4 or 8 rows and each gets a column), fp32 by plain ones.
+// The maximum that weights refer to moves only when a score exceeds it by 2^8 (any reference gives the same quotients): otherwise every
+// tile would rescale the whole of O.
+//
+// Tiles travel global -> LDS by direct 16-byte loads, NST stages; a lane asks for its own token's address, so pages may end anywhere in a tile.
+// 16-byte chunks are permuted within a row (f_k, f_v) so that the fragment reads of 8 or 16 rows fall on different banks.
+//
+// Work.  Lengths are known on the device only.  All (window, head of keys and values) items' tiles form one line, which is cut into equal pieces for
+// `clusters` clusters of NB workgroups (one per block of QB vectors; a cluster's workgroups run on one XCD and read the same tokens at the same
+// time).  Every workgroup finds its piece by a prefix sum over the windows.  Items cut by a piece's border leave partial results (maximum, sum,
+// unscaled O in fp32), which join_kernel adds in the order of the pieces, so that the same call gives the same bits.
+#pragma once
+#include <math.h>
+
+#include "cache.h"
+#include "lds_pipeline.h"
+
+namespace aj {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4))) short i16x4;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
+// DP: head size, padded; WQ x WK waves: WQ blocks of 32 vectors, WK parts of KT tokens of a tile
+template <CacheType TYPE_, int DP_, int WQ_, int WK_, int KT_, int NST_, int PER_CU_>
+struct Form {
+    static constexpr CacheType TYPE = TYPE_;
+    static constexpr int DP = DP_, WQ = WQ_, WK = WK_, KT = KT_, NST = NST_, PER_CU = PER_CU_;
+    static constexpr int KES = TYPE == CACHE_FP8 ? 1 : TYPE == CACHE_F32 ? 4 : 2;
+    static constexpr int WAVES = WQ * WK, THREADS = 64 * WAVES, QB = 32 * WQ, ST = WK * KT;
+    static constexpr int RB = DP * KES, CPR = RB / 16, RPI = 64 / CPR;        // bytes and chunks of a row, rows of a load instruction
+    static constexpr int TILE = ST * RB, STAGE = 2 * TILE;                    // keys, then values
+    static constexpr int NI = TILE / 1024 / WAVES;                            // load instructions of a wave for the keys of a tile (values: the same)
+    static constexpr int NKB = KT / 32, DB = DP / 32, QREGS = TYPE == CACHE_F32 ? DP / 8 : DP / 16;
+    static constexpr int SEG = 2048;                                          // page numbers in LDS
+    static constexpr int MERGE = WK > 1 ? WAVES * DP * 32 * 4 : 0;            // bytes to add up the waves' parts
+    static constexpr int LDS = NST * STAGE > MERGE ? NST * STAGE : MERGE;
+    static_assert(TILE % (1024 * WAVES) == 0 && CPR <= 64 && 2 * NI * (NST - 1) < 64, "whole load instructions, vmcnt");
+};
+
+// chunk permutation of a row of keys / values
+template <class F>
+__device__ __forceinline__ int f_k(int row)
+{
+    return F::RB >= 256 ? row & 15 : F::RB == 128 ? row >> 1 & 7 : row >> 2 & 3;
+}
+template <class F>
+__device__ __forceinline__ int f_v(int row)
+{
+    if (F::TYPE == CACHE_F32) return (row >> 2 & 1) << 3;                                      // tokens 4 apart are read together
+    if (F::TYPE == CACHE_FP8) return f_k<F>(row);
+    return F::RB >= 256 ? (row & 7) << 1 : (row >> 1 & 3) << 1;                                // 32-byte pieces of 8 rows are read together
+}
+
+__device__ __forceinline__ void load_to_lds_16_at(const char *at, uint32_t lds_dst)
+{
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds_dst) : "memory");
+}
+
+// maximum and sum of the lane's value and that of the lane 32 away (swapping the halves of two copies leaves each half's values in both)
+__device__ __forceinline__ float max_halves(float x)
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float sum_halves(float x)
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// V^T as the A operand of a product over 16 tokens: element d = 32 db + lane % 32 of the tokens 16 ks + 4 h + {0..3} and 16 ks + 8 + 4 h + {0..3}.
+// Sixteen lanes give the addresses of 4 (8) rows of 16 elements, in pieces of 8 bytes, and lane i of them gets column i
+template <class F>
+__device__ __forceinline__ bf16x8 values(const char *vt, int ks, int db, int lane)
+{
+    const int h = lane >> 5, part = lane >> 4 & 1, i = lane & 15;
+    if constexpr (F::TYPE == CACHE_BF16) {
+        typedef __attribute__((address_space(3))) i16x4 *at;
+        const int row = 16 * ks + 4 * h + (i >> 2), chunk = (4 * db + 2 * part + (i >> 1 & 1)) ^ f_v<F>(row);
+        const char *p = vt + row * F::RB + chunk * 16 + (i & 1) * 8;
+        const i16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)p), y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p + 8 * F::RB));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        typedef __attribute__((address_space(3))) i32x2 *at;
+        const int j = i >> 1, row = 16 * ks + 4 * h + (j & 3) + 8 * (j >> 2), chunk = (2 * db + part) ^ f_v<F>(row);
+        const i32x2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((at)(vt + row * F::RB + chunk * 16 + (i & 1) * 8));
+        return widen(y[0], y[1]);
+    }
+}
+
+// What a window's tokens look like to its rows
+struct Span {
+    int L, R;         // cached tokens, live rows
+    int hi;           // tokens are t < hi
+    int lo;           // sinks <= t < lo: seen by no row
+    int ns, first, n; // tiles that are visited: 0 .. ns-1, first .. ; n of them in all
+};
+
+template <int ST>
+__device__ __forceinline__ Span span_of(const AttendArgs &a, int b)
+{
+    Span s;
+    s.L = cached_tokens(a.pages, b);
+    s.R = live_rows(a.pages, b);
+    s.lo = s.ns = s.first = 0;
+    const int cap = a.pages.width << a.pages.log_page;
+    s.hi = s.L + s.R < cap ? s.L + s.R : cap;
+    const int end = (s.hi - 1) / ST + 1;
+    s.n = end;
+    if (a.window) {
+        const int lo = s.L - a.window + 1, sk = a.sinks < s.hi ? a.sinks : s.hi;
+        s.lo = lo > 0 ? lo : 0;
+        s.ns = (sk + ST - 1) / ST;
+        s.first = s.lo / ST > s.ns ? s.lo / ST : s.ns;
+        if (s.first > end) s.first = end;
+        s.n = s.ns + end - s.first;
+        if (s.n == 0) s.n = 1, s.first = 0;      // nothing is seen: the rows' zeros have to be written all the same
+    }
+    if (s.R == 0) s.n = 0;
+    return s;
+}
+
+// tiles of all items, and the window that has place w of their line: its number and its first place
+template <int ST, int THREADS>
+struct Line {
+    int *sums;   // LDS, THREADS / 64 + 3
+
+    __device__ __forceinline__ int total(const AttendArgs &a) const
+    {
+        int n = 0;
+        for (int b = threadIdx.x; b < a.pages.B; b += THREADS) n += span_of<ST>(a, b).n;
+#pragma unroll
+        for (int o = 32; o; o /= 2) n += __shfl_xor(n, o);
+        if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) n += sums[w];
+        __syncthreads();
+        return n * a.n_kv;
+    }
+
+    __device__ __forceinline__ void find(const AttendArgs &a, int w, int &b_out, int &start_out) const
+    {
+        int *found = sums + THREADS / 64, carry = 0;
+        for (int base = 0; base < a.pages.B; base += THREADS) {
+            const int b = base + (int)threadIdx.x, mine = b < a.pages.B ? span_of<ST>(a, b).n * a.n_kv : 0;
+            int incl = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                const int y = __shfl_up(incl, o);
+                if ((int)threadIdx.x % 64 >= o) incl += y;
+            }
+            if (threadIdx.x % 64 == 63) sums[threadIdx.x / 64] = incl;
+            if (threadIdx.x == 0) found[0] = -1;
+            __syncthreads();
+            int before = carry, all = 0;
+#pragma unroll
+            for (int v = 0; v < THREADS / 64; ++v) {
+                if (v < (int)threadIdx.x / 64) before += sums[v];
+                all += sums[v];
+            }
+            if (w >= before + incl - mine && w < before + incl) found[0] = b, found[1] = before + incl - mine;
+            __syncthreads();
+            b_out = found[0], start_out = found[1];
+            carry += all;
+            __syncthreads();
+            if (b_out >= 0) break;
+        }
+        b_out = __builtin_amdgcn_readfirstlane(b_out);
+        start_out = __builtin_amdgcn_readfirstlane(start_out);
+    }
+};
+
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+// out and lse of one vector from its unscaled sums
+template <CacheType TYPE>
+__device__ __forceinline__ void finish(const AttendArgs &a, int64_t vec, int d4, f32x4 o, float l)
+{
+    if (4 * d4 >= a.D) return;
+    const float f = l > 0.f || l != l ? a.v_scale / l : 0.f;
+    if constexpr (TYPE == CACHE_F32) {
+        *(f32x4 *)((float *)a.out + vec * a.D + 4 * d4) = f32x4{o[0] * f, o[1] * f, o[2] * f, o[3] * f};
+    } else {
+        bf16x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = (__bf16)(o[i] * f);
+        *(bf16x4 *)((__bf16 *)a.out + vec * a.D + 4 * d4) = y;
+    }
+}
+
+__device__ __forceinline__ void finish_lse(const AttendArgs &a, int64_t vec, float m, float l)
+{
+    // m: the reference of the weights as a power of two
+    if (a.lse) a.lse[vec] = l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * 0.69314718f : -INFINITY;
+}
+
+template <class F>
+__global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PER_CU *F::WAVES / 4) void attend_kernel(AttendArgs a)
+{
+    constexpr int ST = F::ST, RB = F::RB, KT = F::KT, DB = F::DB, NKB = F::NKB, NI = F::NI, QB = F::QB;
+    constexpr bool F32 = F::TYPE == CACHE_F32;
+    __shared__ __attribute__((aligned(1024))) char lds[F::LDS];
+    __shared__ int tab[F::SEG];
+    __shared__ int sums[F::WAVES + 3];
+    __shared__ int wflag[2][F::WAVES];
+    __shared__ float mls[2][F::WK][QB];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
+    const int wq = wave % F::WQ, wk = wave / F::WQ;
+    const int G = a.n_q / a.n_kv, words = (a.pages.rows + 31) / 32;
+    const int cap = a.pages.width << a.pages.log_page, page = 1 << a.pages.log_page;
+
+    // this workgroup's piece of the line of tiles; its block of vectors
+    const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, per_xcd = a.clusters / 8;
+    const int cluster = xcd * per_xcd + place / a.blocks, block = place % a.blocks;
+    const Line<ST, F::THREADS> line{sums};
+    const int total = line.total(a), chunk = (total + a.clusters - 1) / a.clusters;
+    int w = cluster * chunk;
+    const int w_end = w + chunk < total ? w + chunk : total;
+    if (w >= w_end) return;
+    int b, start;
+    line.find(a, w, b, start);
+    Span sp = span_of<ST>(a, b);
+
+    const uint32_t lds0 = lds_offset_of(lds);
+    const float c = a.score_scale, threshold = 8.f / c;
+
+    while (w < w_end) {
+        while (w >= start + sp.n * a.n_kv) {      // (windows without rows have no places)
+            start += sp.n * a.n_kv;
+            ++b;
+            sp = span_of<ST>(a, b);
+        }
+        const int kvh = (w - start) / sp.n, i_first = (w - start) % sp.n;
+        const int i_last = sp.n - i_first < w_end - w ? sp.n : i_first + (w_end - w);     // end of the visits
+        const int item = start + kvh * sp.n;                                              // first place of the item
+        const bool whole = i_first == 0 && i_last == sp.n;
+        w += i_last - i_first;
+        const int nvec = sp.R * G;
+        if (block * QB >= nvec) continue;
+        const int x_last = (block + 1) * QB < nvec ? (block + 1) * QB - 1 : nvec - 1;
+        const int r_first = block * QB / G, r_last = x_last / G;
+
+        // the visits that this block needs: not those behind its last row, nor those before its first row's window
+        int i_begin = i_first, i_end = i_last;
+        {
+            const int hi = sp.L + r_last + 1 < cap ? sp.L + r_last + 1 : cap;
+            const int tile = (hi - 1) / ST, last = tile >= sp.first ? sp.ns + tile - sp.first : tile < sp.ns ? tile : sp.ns - 1;
+            if (i_end > last + 1) i_end = last + 1 > i_begin ? last + 1 : i_begin;
+            if (a.window && !a.pages.depth && i_begin >= sp.ns) {
+                const int lo = sp.L + r_first - a.window + 1, i = sp.ns + lo / ST - sp.first;
+                if (lo > 0 && i > i_begin) i_begin = i < i_end ? i : i_end;
+            }
+        }
+
+        // queries as the B operand: column = vector
+        const int x = block * QB + wq * 32 + col, xc = x < nvec ? x : nvec - 1, r = xc / G, head = kvh * G + xc % G;
+        const bool active = block * QB + wq * 32 < nvec;
+        const int64_t vec = ((int64_t)b * a.pages.rows + r) * a.n_q + head;
+        u32x4 q[F::QREGS];
+        {
+            const char *row = (const char *)a.q + (((int64_t)b * a.pages.rows + r) * a.q_stride + head * a.D) * (F32 ? 4 : 2);
+#pragma unroll
+            for (int s = 0; s < F::QREGS; ++s) {
+                const int d = F32 ? 4 * (2 * s + h) : F::TYPE == CACHE_FP8 ? 16 * (2 * (s / 2) + h) + 8 * (s & 1) : 16 * s + 8 * h;
+                q[s] = d < a.D ? *(const u32x4 *)(row + d * (F32 ? 4 : 2)) : u32x4{0, 0, 0, 0};
+            }
+        }
+        const int my_depth = depth_of(a.pages, b, r);
+        f32x16 acc[DB];
+#pragma unroll
+        for (int i = 0; i < DB; ++i) acc[i] = f32x16{0};
+        float m = -INFINITY, l = 0.f;
+
+        const char *k_head = (const char *)a.k_pool + kvh * a.pages.head_stride, *v_head = (const char *)a.v_pool + kvh * a.pages.head_stride;
+        const int per_tile = page < ST ? ST >> a.pages.log_page : 1, seg_tiles = F::SEG / per_tile;
+        const auto tile_of_visit = [&](int i) { return i < sp.ns ? i : sp.first + i - sp.ns; };
+
+        for (int seg = i_begin; seg < i_end; seg += seg_tiles) {
+            const int seg_end = seg + seg_tiles < i_end ? seg + seg_tiles : i_end;
+            // the segment's page numbers; -1: nowhere
+            __syncthreads();
+            int bad = 0;
+            for (int e = tid; e < (seg_end - seg) * per_tile; e += F::THREADS) {
+                const int t = tile_of_visit(seg + e / per_tile) * ST + (e % per_tile << a.pages.log_page);   // (its first token, or one on its page)
+                int p = -1;
+                if (t < cap) {
+                    p = a.pages.table[(int64_t)b * a.pages.width + (t >> a.pages.log_page)];
+                    if ((uint32_t)p >= (uint32_t)a.pages.n_pages) p = -1;
+                }
+                tab[e] = p;
+                const int until = page < ST ? t + page : t + ST;
+                if (p < 0 && t < sp.hi && !(t >= a.sinks && until <= sp.lo)) bad = 1;
+            }
+            bad = __any(bad);
+            if (lane == 0) wflag[1][wave] = bad;
+            __syncthreads();
+            bad = 0;
+#pragma unroll
+            for (int v = 0; v < F::WAVES; ++v) bad |= wflag[1][v];
+
+            const auto page_of = [&](int i, int row) { return tab[(i - seg) * per_tile + (page < ST ? row >> a.pages.log_page : 0)]; };
+            const auto issue = [&](int i, int stage) {
+                const int t0 = tile_of_visit(i) * ST;
+                int64_t off[NI];
+#pragma unroll
+                for (int n = 0; n < NI; ++n) {
+                    const int row = (wave * NI + n) * F::RPI + lane / F::CPR, p = page_of(i, row);
+                    // (a token that is nowhere reads slot 0 of the pool; so does one behind the last)
+                    off[n] = p >= 0 && t0 + row < sp.hi ? p * a.pages.page_stride + ((t0 + row) & (page - 1)) * a.pages.slot_stride : 0;
+                }
+#pragma unroll
+                for (int n = 0; n < NI; ++n) {
+                    const int row = (wave * NI + n) * F::RPI + lane / F::CPR, pc = lane % F::CPR;
+                    int ck = pc ^ f_k<F>(row), cv = pc ^ f_v<F>(row);
+                    if (ck * 16 >= a.D * F::KES) ck = 0;      // padding: the query is zero there, and so is what is written
+                    if (cv * 16 >= a.D * F::KES) cv = 0;
+                    const uint32_t dst = lds0 + stage * F::STAGE + (wave * NI + n) * 1024;
+                    load_to_lds_16_at(k_head + off[n] + ck * 16, dst);
+                    load_to_lds_16_at(v_head + off[n] + cv * 16, dst + F::TILE);
+                }
+            };
+
+#pragma unroll
+            for (int s = 0; s < F::NST - 1; ++s)
+                if (seg + s < seg_end) issue(seg + s, s);
+            int stage = 0;
+            for (int i = seg; i < seg_end; ++i) {
+                // tile i has landed, for every wave, and nobody reads the stage before it any more
+                if (F::NST > 3 && i + 2 < seg_end) wait_vm_lgkm_and_barrier<(F::NST > 3 ? 4 * NI : 0)>();
+                else if (F::NST > 2 && i + 1 < seg_end) wait_vm_lgkm_and_barrier<(F::NST > 2 ? 2 * NI : 0)>();
+                else wait_vm_lgkm_and_barrier<0>();
+                if (i + F::NST - 1 < seg_end) issue(i + F::NST - 1, stage == 0 ? F::NST - 1 : stage - 1);
+
+                const int t_tile = tile_of_visit(i) * ST;
+                const bool full = !bad && t_tile + ST <= sp.L && t_tile + ST <= sp.hi &&
+                                  (!a.window || t_tile + ST <= a.sinks || sp.L + r_last - t_tile < a.window);
+                char *tile = lds + stage * F::STAGE;
+                bool poisoned = false;
+                if (!full) {
+                    // values of tokens that nobody sees count as zero whatever they are; and look for values that are not finite
+                    int odd = 0;
+                    for (int e = tid; e < ST * F::CPR; e += F::THREADS) {
+                        const int row = e / F::CPR, t = t_tile + row;
+                        const bool dead = t >= sp.hi || (a.window && t >= a.sinks && t < sp.lo) || page_of(i, row) < 0;
+                        u32x4 *at = (u32x4 *)(tile + F::TILE + e * 16);
+                        if (dead) *at = u32x4{0, 0, 0, 0};
+                        else if (sp.R > 1) {
+                            const u32x4 y = *at;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if constexpr (F32) odd |= (y[j] & 0x7f800000u) == 0x7f800000u;
+                                else if constexpr (F::TYPE == CACHE_BF16) odd |= (y[j] & 0x7f80u) == 0x7f80u || (y[j] & 0x7f800000u) == 0x7f800000u;
+                                else odd |= (((y[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                            }
+                        }
+                    }
+                    odd = __any(odd);
+                    if (lane == 0) wflag[0][wave] = odd;
+                    __syncthreads();
+#pragma unroll
+                    for (int v = 0; v < F::WAVES; ++v) poisoned |= wflag[0][v] != 0;
+                }
+
+                if (active) {
+                    const char *kt = tile + wk * KT * RB, *vt = tile + F::TILE + wk * KT * RB;
+                    const int t0 = t_tile + wk * KT;
+                    f32x16 s[NKB];
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb) {
+                        s[kb] = f32x16{0};
+                        const char *row = kt + (kb * 32 + col) * RB;
+                        const int f = f_k<F>(col);
+#pragma unroll
+                        for (int ks = 0; ks < RB / 32; ++ks) {
+                            const u32x4 y = *(const u32x4 *)(row + (((2 * ks + h) ^ f) * 16));
+                            if constexpr (F32) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(y[e]), __uint_as_float(q[ks][e]), s[kb], 0, 0, 0);
+                            } else if constexpr (F::TYPE == CACHE_BF16) {
+                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y), __builtin_bit_cast(bf16x8, q[ks]), s[kb], 0, 0, 0);
+                            } else {
+                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(y[0], y[1]), __builtin_bit_cast(bf16x8, q[2 * ks]), s[kb], 0, 0, 0);
+                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(y[2], y[3]), __builtin_bit_cast(bf16x8, q[2 * ks + 1]), s[kb], 0, 0, 0);
+                            }
+                        }
+                    }
+
+                    uint32_t vis[NKB];
+                    if (!full) {
+#pragma unroll
+                        for (int kb = 0; kb < NKB; ++kb) {
+                            const int t = t0 + 32 * kb;
+                            uint32_t y = below(sp.hi - t) & below(sp.L + r + 1 - t);
+                            const uint32_t old = below(sp.L - t);
+                            if (a.mask && old != ~0u) {
+                                const uint32_t *mw = a.mask + ((int64_t)b * a.pages.rows + r) * words;
+                                const int at = t - sp.L, wd = at >> 5, sh = at & 31;      // (at > -32)
+                                const uint32_t m0 = wd >= 0 && wd < words ? mw[wd] : 0u, m1 = wd + 1 < words ? mw[wd + 1] : 0u;
+                                y &= old | (sh ? m0 >> sh | m1 << (32 - sh) : m0);
+                            }
+                            if (a.window) {
+                                const uint32_t sunk = below(a.sinks - t), near = ~below(sp.L + my_depth - a.window + 1 - t);
+                                if (!a.pages.depth) {
+                                    y &= sunk | near;
+                                } else {
+                                    y &= ~old | sunk | near;
+                                    if (my_depth >= a.window)      // new rows further away than the window
+                                        for (uint32_t left = y & ~old; left; left &= left - 1) {
+                                            const int e = __ffs(left) - 1, d = depth_of(a.pages, b, t + e - sp.L);
+                                            if (my_depth - d >= a.window && sp.L + d >= a.sinks) y &= ~(1u << e);
+                                        }
+                                }
+                            }
+                            if (bad)
+                                for (int e = 0; e < 32; ++e)
+                                    if (page_of(i, wk * KT + kb * 32 + e) < 0) y &= ~(1u << e);
+                            vis[kb] = y;
+                            y >>= 4 * h;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                s[kb][e] = y >> (e % 4 + 8 * (e / 4)) & 1 ? s[kb][e] : -INFINITY;
+                        }
+                    }
+
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+                    mx = max_halves(mx);
+                    if (__any(mx > m + threshold)) {
+                        const float mn = fmaxf(m, mx), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
+#pragma unroll
+                        for (int i = 0; i < DB; ++i)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) acc[i][e] *= f;
+                        l *= f;
+                        m = mn;
+                    }
+                    const float base = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c, -base));
+                            l += s[kb][e];
+                        }
+                    }
+
+                    // O^T += V^T P^T
+                    if constexpr (F32) {
+                        const auto value = [&](int kb, int e, int db) {
+                            const int row = kb * 32 + e % 4 + 8 * (e / 4) + 4 * h;
+                            return *(const float *)(vt + row * RB + (((8 * db + (col >> 2)) ^ (h << 3)) * 16) + (col & 3) * 4);
+                        };
+                        if (!poisoned) {
+#pragma unroll
+                            for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                                for (int e = 0; e < 16; ++e)
+#pragma unroll
+                                    for (int db = 0; db < DB; ++db)
+                                        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(kb, e, db), s[kb][e], acc[db], 0, 0, 0);
+                        } else {
+                            // some values are not finite: a token at a time, and only for the vectors that see it
+#pragma unroll
+                            for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                                for (int e = 0; e < 16; ++e)
+                                    for (int one = 0; one < 2; ++one) {
+                                        const bool seen = vis[kb] >> (e % 4 + 8 * (e / 4) + 4 * one) & 1;
+#pragma unroll
+                                        for (int db = 0; db < DB; ++db) {
+                                            const f32x16 z =
+                                                __builtin_amdgcn_mfma_f32_32x32x2f32(h == one ? value(kb, e, db) : 0.f, s[kb][e], acc[db], 0, 0, 0);
+#pragma unroll
+                                            for (int j = 0; j < 16; ++j) acc[db][j] = seen ? z[j] : acc[db][j];
+                                        }
+                                    }
+                        }
+                    } else {
+#pragma unroll
+                        for (int ks = 0; ks < KT / 16; ++ks) {
+                            bf16x8 p;      // weights lose at most half a step of bf16, 2^-8 of each: as the products' operand they have to
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[ks / 2][8 * (ks & 1) + e];
+                            bf16x8 y[DB];
+#pragma unroll
+                            for (int db = 0; db < DB; ++db) y[db] = values<F>(vt, ks, db, lane);
+                            if (!poisoned) {
+#pragma unroll
+                                for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[db], p, acc[db], 0, 0, 0);
+                            } else {
+                                // some values are not finite: a token at a time, and only for the vectors that see it
+                                for (int one = 0; one < 16; ++one) {
+                                    const int place = (one & 3) + (one >> 3) * 4, half = one >> 2 & 1;
+                                    const bool seen = vis[ks / 2] >> (16 * (ks & 1) + one) & 1;
+#pragma unroll
+                                    for (int db = 0; db < DB; ++db) {
+                                        bf16x8 y1;
+#pragma unroll
+                                        for (int e = 0; e < 8; ++e) y1[e] = h == half && e == place ? y[db][e] : (__bf16)0.f;
+                                        const f32x16 z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y1, p, acc[db], 0, 0, 0);
+#pragma unroll
+                                        for (int j = 0; j < 16; ++j) acc[db][j] = seen ? z[j] : acc[db][j];
+                                    }
+                                }
+                            }
+                        }
+                    }
+                }
+                stage = stage + 1 == F::NST ? 0 : stage + 1;
+            }
+        }
+
+        // the halves' sums; the waves that shared the block's tokens
+        l = sum_halves(l);
+        const int64_t unit = ((int64_t)cluster * 2 + (item > cluster * chunk)) * a.blocks + block;
+        float *part_o = a.part_o + unit * QB * F::DP;
+        float2 *part_ml = a.part_ml + unit * QB;
+        if constexpr (F::WK == 1) {
+            if (x < nvec) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x4 o = {acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]};
+                        const int d4 = 8 * db + 2 * e + h;
+                        if (whole) finish<F::TYPE>(a, vec, d4, o, l);
+                        else *(f32x4 *)(part_o + ((int64_t)d4 * QB + wq * 32 + col) * 4) = o;
+                    }
+                if (h == 0) {
+                    if (whole) finish_lse(a, vec, m * c, l);
+                    else part_ml[wq * 32 + col] = float2{m * c, l};
+                }
+            }
+        } else {
+            __syncthreads();      // the stages are free
+            if (h == 0) mls[0][wk][wq * 32 + col] = m, mls[1][wk][wq * 32 + col] = l;
+            __syncthreads();
+            float top = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < F::WK; ++v) top = fmaxf(top, mls[0][v][wq * 32 + col]);
+            const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
+            float *merge = (float *)lds;      // [WK][DP/4][QB][4]
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(f32x4 *)(merge + ((wk * (F::DP / 4) + 8 * db + 2 * e + h) * QB + wq * 32 + col) * 4) =
+                        f32x4{acc[db][4 * e] * mine, acc[db][4 * e + 1] * mine, acc[db][4 * e + 2] * mine, acc[db][4 * e + 3] * mine};
+            __syncthreads();
+            for (int e = tid; e < F::DP / 4 * QB; e += F::THREADS) {
+                const int d4 = e / QB, xl = e % QB, xx = block * QB + xl;
+                if (xx >= nvec) continue;
+                float tm = -INFINITY, tl = 0.f;
+#pragma unroll
+                for (int v = 0; v < F::WK; ++v) tm = fmaxf(tm, mls[0][v][xl]);
+                f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+                for (int v = 0; v < F::WK; ++v) {
+                    const float mv = mls[0][v][xl];
+                    tl += mls[1][v][xl] * (mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mv - tm) * c));
+                    o += *(const f32x4 *)(merge + ((v * (F::DP / 4) + d4) * QB + xl) * 4);
+                }
+                const int64_t vx = ((int64_t)b * a.pages.rows + xx / G) * a.n_q + kvh * G + xx % G;
+                if (whole) finish<F::TYPE>(a, vx, d4, o, tl);
+                else *(f32x4 *)(part_o + (int64_t)e * 4) = o;
+                if (d4 == 0) {
+                    if (whole) finish_lse(a, vx, tm * c, tl);
+                    else part_ml[xl] = float2{tm * c, tl};
+                }
+            }
+            // (the barrier before the next item's page numbers keeps its loads out of `merge`)
+        }
+    }
+}
+
+// Adds the parts of the item that is cut at the border between clusters c and c + 1 for the first time, c = blockIdx.x
+template <class F>
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a)
+{
+    constexpr int QB = F::QB, ND = 256 / QB;
+    __shared__ int sums[256 / 64 + 3];
+    const Line<F::ST, 256> line{sums};
+    const int total = line.total(a), chunk = (total + a.clusters - 1) / a.clusters;
+    const int border = ((int)blockIdx.x + 1) * chunk, block = blockIdx.y;
+    if (border >= total) return;
+    int b, start;
+    line.find(a, border, b, start);
+    const Span sp = span_of<F::ST>(a, b);
+    const int kvh = (border - start) / sp.n, item = start + kvh * sp.n;
+    if (item == border || item / chunk != (int)blockIdx.x) return;      // not cut here, or not for the first time
+    const int last = (item + sp.n - 1) / chunk;
+    const int G = a.n_q / a.n_kv, nvec = sp.R * G, xl = threadIdx.x % QB, x = block * QB + xl, d4 = blockIdx.z * ND + threadIdx.x / QB;
+    if (x >= nvec || 4 * d4 >= a.D) return;
+    const auto unit = [&](int c) { return ((int64_t)c * 2 + (item > c * chunk)) * a.blocks + block; };
+    float m = -INFINITY, l = 0.f;
+    for (int c = blockIdx.x; c <= last; ++c) m = fmaxf(m, a.part_ml[unit(c) * QB + xl].x);
+    f32x4 o = {0, 0, 0, 0};
+    for (int c = blockIdx.x; c <= last; ++c) {
+        const float2 ml = a.part_ml[unit(c) * QB + xl];
+        const f32x4 y = *(const f32x4 *)(a.part_o + (unit(c) * F::DP / 4 + d4) * QB * 4 + xl * 4);
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+        l += ml.y * f;
+        o += y * f;
+    }
+    const int64_t vec = ((int64_t)b * a.pages.rows + x / G) * a.n_q + kvh * G + x % G;
+    finish<F::TYPE>(a, vec, d4, o, l);
+    if (d4 == 0) finish_lse(a, vec, m, l);
+}
+
+template <class F>
+hipError_t launch_attend(const AttendArgs &a, hipStream_t s)
+{
+    attend_kernel<F><<<a.clusters * a.blocks, F::THREADS, 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    join_kernel<F><<<dim3(a.clusters - 1, a.blocks, F::DP / 4 / (256 / F::QB)), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <class F>
+AttendPlan plan_attend(int vectors, int num_cus)
+{
+    AttendPlan p;
+    p.vectors = F::QB;
+    p.tokens = F::ST;
+    p.blocks = (vectors + F::QB - 1) / F::QB;
+    const int per_xcd = num_cus / 8 * F::PER_CU / p.blocks;
+    p.clusters = 8 * (per_xcd < 1 ? 1 : per_xcd);
+    p.part_floats = (size_t)p.clusters * 2 * p.blocks * F::QB * F::DP;
+    return p;
+}
+
+}  // namespace aj

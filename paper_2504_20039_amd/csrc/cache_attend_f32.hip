@@ -1,0 +1,36 @@
+// Attention over the paged cache, fp32 storage: the forms that are built (cache_attend.h)
+#include "cache_attend.h"
+
+namespace aj {
+
+template <int DP, bool FEW> struct Choice;
+template <> struct Choice<64, true> { typedef Form<CACHE_F32, 64, 1, 4, 32, 2, 1> F; };
+template <> struct Choice<128, true> { typedef Form<CACHE_F32, 128, 1, 2, 32, 2, 1> F; };
+template <> struct Choice<256, true> { typedef Form<CACHE_F32, 256, 4, 1, 32, 2, 1> F; };
+template <> struct Choice<64, false> { typedef Form<CACHE_F32, 64, 4, 1, 64, 2, 2> F; };
+template <> struct Choice<128, false> { typedef Form<CACHE_F32, 128, 4, 1, 64, 2, 1> F; };
+template <> struct Choice<256, false> { typedef Form<CACHE_F32, 256, 4, 1, 32, 2, 1> F; };
+
+template <int DP>
+static hipError_t launch(bool few, const AttendArgs &a, hipStream_t s)
+{
+    return few ? launch_attend<typename Choice<DP, true>::F>(a, s) : launch_attend<typename Choice<DP, false>::F>(a, s);
+}
+
+hipError_t cache_attend_f32(bool few, const AttendArgs &a, hipStream_t s)
+{
+    return a.D <= 64 ? launch<64>(few, a, s) : a.D <= 128 ? launch<128>(few, a, s) : launch<256>(few, a, s);
+}
+
+template <int DP>
+static AttendPlan plan(int vectors, int num_cus)
+{
+    return vectors <= 32 ? plan_attend<typename Choice<DP, true>::F>(vectors, num_cus) : plan_attend<typename Choice<DP, false>::F>(vectors, num_cus);
+}
+
+AttendPlan cache_attend_plan_f32(int D, int vectors, int num_cus)
+{
+    return D <= 64 ? plan<64>(vectors, num_cus) : D <= 128 ? plan<128>(vectors, num_cus) : plan<256>(vectors, num_cus);
+}
+
+}  // namespace aj
