@@ -111,6 +111,14 @@ __device__ __forceinline__ bf16x8 values(const char *vt, int ks, int db, int lan
     }
 }
 
+// Keeps what is computed from x where it is written: what is needed once per tile or per item would otherwise be computed ahead of the loops and take
+// registers throughout
+__device__ __forceinline__ int here(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // What a window's tokens look like to its rows
 struct Span {
     int L, R;         // cached tokens, live rows
@@ -194,6 +202,20 @@ struct Line {
         start_out = __builtin_amdgcn_readfirstlane(start_out);
     }
 };
+
+// four consecutive elements of a row of values
+template <class F>
+__device__ __forceinline__ f32x4 four(const char *at)
+{
+    if constexpr (F::TYPE == CACHE_F32) return *(const f32x4 *)at;
+    else if constexpr (F::TYPE == CACHE_BF16) {
+        const bf16x4 y = *(const bf16x4 *)at;
+        return f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+    } else {
+        const bf16x8 y = widen(*(const uint32_t *)at, 0);
+        return f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+    }
+}
 
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
@@ -279,7 +301,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
         }
 
         // queries as the B operand: column = vector
-        const int x = block * QB + wq * 32 + col, xc = x < nvec ? x : nvec - 1, r = xc / G, head = kvh * G + xc % G;
+        const int x = block * QB + wq * 32 + col, xc = x < nvec ? x : nvec - 1, r = xc / G, row_of_lane = r, head = kvh * G + xc % G;
         const bool active = block * QB + wq * 32 < nvec;
         const int64_t vec = ((int64_t)b * a.pages.rows + r) * a.n_q + head;
         u32x4 q[F::QREGS];
@@ -326,20 +348,20 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 
             const auto page_of = [&](int i, int row) { return tab[(i - seg) * per_tile + (page < ST ? row >> a.pages.log_page : 0)]; };
             const auto issue = [&](int i, int stage) {
-                const int t0 = tile_of_visit(i) * ST;
+                const int t0 = tile_of_visit(i) * ST, ln = here(lane), row0 = wave * NI * F::RPI + ln / F::CPR, pc = ln % F::CPR;
                 int64_t off[NI];
 #pragma unroll
                 for (int n = 0; n < NI; ++n) {
-                    const int row = (wave * NI + n) * F::RPI + lane / F::CPR, p = page_of(i, row);
-                    // (a token that is nowhere reads slot 0 of the pool; so does one behind the last)
-                    off[n] = p >= 0 && t0 + row < sp.hi ? p * a.pages.page_stride + ((t0 + row) & (page - 1)) * a.pages.slot_stride : 0;
+                    // a token that is nowhere reads slot 0 of page 0; so does one behind the last
+                    const int row = row0 + n * F::RPI, p = page_of(i, row), keep = (p >= 0) & (t0 + row < sp.hi) ? -1 : 0;
+                    off[n] = (p & keep) * a.pages.page_stride + ((t0 + row) & (page - 1) & keep) * a.pages.slot_stride;
                 }
 #pragma unroll
                 for (int n = 0; n < NI; ++n) {
-                    const int row = (wave * NI + n) * F::RPI + lane / F::CPR, pc = lane % F::CPR;
+                    const int row = row0 + n * F::RPI;
                     int ck = pc ^ f_k<F>(row), cv = pc ^ f_v<F>(row);
-                    if (ck * 16 >= a.D * F::KES) ck = 0;      // padding: the query is zero there, and so is what is written
-                    if (cv * 16 >= a.D * F::KES) cv = 0;
+                    ck = ck * 16 >= a.D * F::KES ? 0 : ck;      // padding: the query is zero there, and so is what is written
+                    cv = cv * 16 >= a.D * F::KES ? 0 : cv;
                     const uint32_t dst = lds0 + stage * F::STAGE + (wave * NI + n) * 1024;
                     load_to_lds_16_at(k_head + off[n] + ck * 16, dst);
                     load_to_lds_16_at(v_head + off[n] + cv * 16, dst + F::TILE);
@@ -365,7 +387,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                 if (!full) {
                     // values of tokens that nobody sees count as zero whatever they are; and look for values that are not finite
                     int odd = 0;
-                    for (int e = tid; e < ST * F::CPR; e += F::THREADS) {
+                    for (int e = here(tid); e < ST * F::CPR; e += F::THREADS) {
                         const int row = e / F::CPR, t = t_tile + row;
                         const bool dead = t >= sp.hi || (a.window && t >= a.sinks && t < sp.lo) || page_of(i, row) < 0;
                         u32x4 *at = (u32x4 *)(tile + F::TILE + e * 16);
@@ -392,31 +414,43 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     const int t0 = t_tile + wk * KT;
                     f32x16 s[NKB];
 #pragma unroll
-                    for (int kb = 0; kb < NKB; ++kb) {
-                        s[kb] = f32x16{0};
-                        const char *row = kt + (kb * 32 + col) * RB;
-                        const int f = f_k<F>(col);
+                    for (int kb = 0; kb < NKB; ++kb) s[kb] = f32x16{0};
+                    // fragments are asked for two steps ahead; the barriers keep the compiler from asking for all of them at once, which
+                    // would take more registers than there are
+                    constexpr int KS = RB / 32, AHEAD = 2;
+                    u32x4 y[AHEAD + 1][NKB];
+                    const auto ask = [&](int ks) {
 #pragma unroll
-                        for (int ks = 0; ks < RB / 32; ++ks) {
-                            const u32x4 y = *(const u32x4 *)(row + (((2 * ks + h) ^ f) * 16));
+                        for (int kb = 0; kb < NKB; ++kb) y[ks % (AHEAD + 1)][kb] = *(const u32x4 *)(kt + (kb * 32 + col) * RB + (((2 * ks + h) ^ f_k<F>(col)) * 16));
+                    };
+#pragma unroll
+                    for (int ks = 0; ks < AHEAD && ks < KS; ++ks) ask(ks);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        if (ks + AHEAD < KS) ask(ks + AHEAD);
+#pragma unroll
+                        for (int kb = 0; kb < NKB; ++kb) {
+                            const u32x4 z = y[ks % (AHEAD + 1)][kb];
                             if constexpr (F32) {
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
-                                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(y[e]), __uint_as_float(q[ks][e]), s[kb], 0, 0, 0);
+                                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(z[e]), __uint_as_float(q[ks][e]), s[kb], 0, 0, 0);
                             } else if constexpr (F::TYPE == CACHE_BF16) {
-                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y), __builtin_bit_cast(bf16x8, q[ks]), s[kb], 0, 0, 0);
+                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), __builtin_bit_cast(bf16x8, q[ks]), s[kb], 0, 0, 0);
                             } else {
-                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(y[0], y[1]), __builtin_bit_cast(bf16x8, q[2 * ks]), s[kb], 0, 0, 0);
-                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(y[2], y[3]), __builtin_bit_cast(bf16x8, q[2 * ks + 1]), s[kb], 0, 0, 0);
+                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(z[0], z[1]), __builtin_bit_cast(bf16x8, q[2 * ks]), s[kb], 0, 0, 0);
+                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(z[2], z[3]), __builtin_bit_cast(bf16x8, q[2 * ks + 1]), s[kb], 0, 0, 0);
                             }
                         }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
 
                     uint32_t vis[NKB];
                     if (!full) {
 #pragma unroll
                         for (int kb = 0; kb < NKB; ++kb) {
-                            const int t = t0 + 32 * kb;
+                            const int t = t0 + 32 * kb, r = here(row_of_lane);
                             uint32_t y = below(sp.hi - t) & below(sp.L + r + 1 - t);
                             const uint32_t old = below(sp.L - t);
                             if (a.mask && old != ~0u) {
@@ -475,64 +509,62 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     }
 
                     // O^T += V^T P^T
-                    if constexpr (F32) {
-                        const auto value = [&](int kb, int e, int db) {
-                            const int row = kb * 32 + e % 4 + 8 * (e / 4) + 4 * h;
-                            return *(const float *)(vt + row * RB + (((8 * db + (col >> 2)) ^ (h << 3)) * 16) + (col & 3) * 4);
-                        };
-                        if (!poisoned) {
+                    if (poisoned) {
+                        // some values are not finite: a token at a time, and only for the vectors that see it
+                        for (int e = 0; e < KT; ++e) {
+                            const int h = here(lane) >> 5;
+                            const int from = e % 32 % 4 + 4 * (e % 32 / 8);      // the register and (below) the half that have its weight
+                            float p = 0.f;
+                            uint32_t seen = 0;
 #pragma unroll
-                            for (int kb = 0; kb < NKB; ++kb)
+                            for (int kb = 0; kb < NKB; ++kb) {
+                                if (kb == e / 32) seen = vis[kb] >> (e % 32) & 1;
 #pragma unroll
-                                for (int e = 0; e < 16; ++e)
+                                for (int j = 0; j < 16; ++j) p = kb == e / 32 && j == from ? s[kb][j] : p;
+                            }
+                            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(p), __float_as_uint(p), false, false);
+                            p = __uint_as_float(e >> 2 & 1 ? both[1] : both[0]);
+                            const char *row = vt + e * RB;
+                            const int f = f_v<F>(wk * KT + e);
 #pragma unroll
-                                    for (int db = 0; db < DB; ++db)
-                                        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(kb, e, db), s[kb][e], acc[db], 0, 0, 0);
-                        } else {
-                            // some values are not finite: a token at a time, and only for the vectors that see it
+                            for (int db = 0; db < DB; ++db)
 #pragma unroll
-                            for (int kb = 0; kb < NKB; ++kb)
+                                for (int g = 0; g < 4; ++g) {
+                                    const int at = (32 * db + 8 * g + 4 * h) * F::KES;
+                                    const f32x4 y = four<F>(row + ((at / 16) ^ f) * 16 + at % 16);
 #pragma unroll
-                                for (int e = 0; e < 16; ++e)
-                                    for (int one = 0; one < 2; ++one) {
-                                        const bool seen = vis[kb] >> (e % 4 + 8 * (e / 4) + 4 * one) & 1;
-#pragma unroll
-                                        for (int db = 0; db < DB; ++db) {
-                                            const f32x16 z =
-                                                __builtin_amdgcn_mfma_f32_32x32x2f32(h == one ? value(kb, e, db) : 0.f, s[kb][e], acc[db], 0, 0, 0);
-#pragma unroll
-                                            for (int j = 0; j < 16; ++j) acc[db][j] = seen ? z[j] : acc[db][j];
-                                        }
-                                    }
+                                    for (int j = 0; j < 4; ++j) acc[db][4 * g + j] = seen ? fmaf(p, y[j], acc[db][4 * g + j]) : acc[db][4 * g + j];
+                                }
                         }
-                    } else {
+                    } else if constexpr (F32) {
 #pragma unroll
-                        for (int ks = 0; ks < KT / 16; ++ks) {
+                        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                float y[DB];
+#pragma unroll
+                                for (int db = 0; db < DB; ++db)
+                                    y[db] = *(const float *)(vt + (kb * 32 + e % 4 + 8 * (e / 4) + 4 * h) * RB + (((8 * db + (col >> 2)) ^ (h << 3)) * 16) + (col & 3) * 4);
+#pragma unroll
+                                for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[db], s[kb][e], acc[db], 0, 0, 0);
+                            }
+                    } else {
+                        constexpr int KS = KT / 16;
+                        bf16x8 y[2][DB];
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) y[0][db] = values<F>(vt, 0, db, lane);
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) {
                             bf16x8 p;      // weights lose at most half a step of bf16, 2^-8 of each: as the products' operand they have to
 #pragma unroll
                             for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[ks / 2][8 * (ks & 1) + e];
-                            bf16x8 y[DB];
+                            if (ks + 1 < KS) {
 #pragma unroll
-                            for (int db = 0; db < DB; ++db) y[db] = values<F>(vt, ks, db, lane);
-                            if (!poisoned) {
-#pragma unroll
-                                for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[db], p, acc[db], 0, 0, 0);
-                            } else {
-                                // some values are not finite: a token at a time, and only for the vectors that see it
-                                for (int one = 0; one < 16; ++one) {
-                                    const int place = (one & 3) + (one >> 3) * 4, half = one >> 2 & 1;
-                                    const bool seen = vis[ks / 2] >> (16 * (ks & 1) + one) & 1;
-#pragma unroll
-                                    for (int db = 0; db < DB; ++db) {
-                                        bf16x8 y1;
-#pragma unroll
-                                        for (int e = 0; e < 8; ++e) y1[e] = h == half && e == place ? y[db][e] : (__bf16)0.f;
-                                        const f32x16 z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y1, p, acc[db], 0, 0, 0);
-#pragma unroll
-                                        for (int j = 0; j < 16; ++j) acc[db][j] = seen ? z[j] : acc[db][j];
-                                    }
-                                }
+                                for (int db = 0; db < DB; ++db) y[(ks + 1) & 1][db] = values<F>(vt, ks + 1, db, lane);
                             }
+#pragma unroll
+                            for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[ks & 1][db], p, acc[db], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
                     }
                 }
@@ -546,6 +578,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
         float *part_o = a.part_o + unit * QB * F::DP;
         float2 *part_ml = a.part_ml + unit * QB;
         if constexpr (F::WK == 1) {
+            const int col = here(lane) & 31, h = here(lane) >> 5;
             if (x < nvec) {
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
@@ -569,15 +602,15 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 #pragma unroll
             for (int v = 0; v < F::WK; ++v) top = fmaxf(top, mls[0][v][wq * 32 + col]);
             const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
-            float *merge = (float *)lds;      // [WK][DP/4][QB][4]
+            float *merge = (float *)lds + ((wk * (F::DP / 4) + (here(lane) >> 5)) * QB + wq * 32 + (here(lane) & 31)) * 4;      // [WK][DP/4][QB][4]
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    *(f32x4 *)(merge + ((wk * (F::DP / 4) + 8 * db + 2 * e + h) * QB + wq * 32 + col) * 4) =
+                    *(f32x4 *)(merge + (8 * db + 2 * e) * QB * 4) =
                         f32x4{acc[db][4 * e] * mine, acc[db][4 * e + 1] * mine, acc[db][4 * e + 2] * mine, acc[db][4 * e + 3] * mine};
             __syncthreads();
-            for (int e = tid; e < F::DP / 4 * QB; e += F::THREADS) {
+            for (int e = here(tid); e < F::DP / 4 * QB; e += F::THREADS) {
                 const int d4 = e / QB, xl = e % QB, xx = block * QB + xl;
                 if (xx >= nvec) continue;
                 float tm = -INFINITY, tl = 0.f;
@@ -588,7 +621,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                 for (int v = 0; v < F::WK; ++v) {
                     const float mv = mls[0][v][xl];
                     tl += mls[1][v][xl] * (mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mv - tm) * c));
-                    o += *(const f32x4 *)(merge + ((v * (F::DP / 4) + d4) * QB + xl) * 4);
+                    o += *(const f32x4 *)((float *)lds + ((v * (F::DP / 4) + d4) * QB + xl) * 4);
                 }
                 const int64_t vx = ((int64_t)b * a.pages.rows + xx / G) * a.n_q + kvh * G + xx % G;
                 if (whole) finish<F::TYPE>(a, vx, d4, o, tl);
