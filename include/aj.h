@@ -304,8 +304,8 @@ typedef struct {
     int32_t sinks;        /* ... the tokens at positions below `sinks` (>= 0; must be 0 when window is 0) */
     int32_t rot_dim;      /* elements of a head that are rotated: a multiple of 16 up to head_dim; 0: none */
     int32_t rope;         /* AJ_ROPE_HALF: element i pairs with i + rot_dim/2; AJ_ROPE_INTERLEAVED: 2i with 2i + 1 */
-    int64_t page_stride, slot_stride, head_stride; /* of the pools, in elements; all three 0: as above.  Multiples of 16 bytes, > 0, and no two
-                             tokens' heads may overlap */
+    int64_t page_stride, slot_stride, head_stride; /* of the pools, in elements; all three 0: as above.  Multiples of 16 bytes, >= head_dim,
+                             page_size * slot_stride under 4 GiB, and no two tokens' heads may overlap */
     int64_t qkv_stride;   /* elements between rows of q, k and v of aj_cache_append (a fused projection); 0: n_q * head_dim and n_kv * head_dim */
     int64_t q_stride;     /* elements between rows of q_out and of aj_cache_attend's q; 0: n_q * head_dim */
     int32_t flags;        /* 0 */

@@ -67,19 +67,22 @@ struct AttendArgs {
     int64_t q_stride;      // elements
     float score_scale;     // scale * k_scale * log2(e): weights are powers of two
     float v_scale;
-    // the line of tiles is cut into `clusters` pieces of `blocks` workgroups; partial results of two items per piece
-    int clusters, blocks;
-    float *part_o;         // [clusters][2][blocks][head size / 4][vectors of a block][4]
-    float2 *part_ml;       // [clusters][2][blocks][vectors of a block]
+    // the line of tiles is cut into `clusters` pieces; a cluster has a workgroup for each of `heads` heads of keys and values and `blocks` blocks of
+    // vectors; groups = n_kv / heads.  Partial results of two items per piece
+    int clusters, heads, groups, blocks;
+    int least;             // tiles of a piece at least
+    float *part_o;         // [clusters][2][heads][blocks][head size / 4][vectors of a block][4]
+    float2 *part_ml;       // [clusters][2][heads][blocks][vectors of a block]
+    int *arrived;          // [clusters][heads][blocks], zero between calls
 };
 struct AttendPlan {
     int vectors, tokens;   // query vectors (rows x query heads of one head of keys) of a workgroup, tokens of a tile
-    int blocks, clusters;
-    size_t part_floats;
+    int blocks, heads, clusters;
+    size_t parts, part_size;   // partial results, one per vector, and their floats
 };
-AttendPlan cache_attend_plan_bf16(int D, int vectors, int num_cus);
-AttendPlan cache_attend_plan_fp8(int D, int vectors, int num_cus);
-AttendPlan cache_attend_plan_f32(int D, int vectors, int num_cus);
+AttendPlan cache_attend_plan_bf16(int D, int vectors, int n_kv, int num_cus);
+AttendPlan cache_attend_plan_fp8(int D, int vectors, int n_kv, int num_cus);
+AttendPlan cache_attend_plan_f32(int D, int vectors, int n_kv, int num_cus);
 // few: up to 32 vectors, which the waves of a workgroup share, each with tokens of its own; otherwise a wave has vectors of its own
 hipError_t cache_attend_bf16(bool few, const AttendArgs &a, hipStream_t s);
 hipError_t cache_attend_fp8(bool few, const AttendArgs &a, hipStream_t s);

@@ -17,6 +17,7 @@ struct aj_cache {
     AttendPlan plan;
     float *part_o;         // partial results of aj_cache_attend
     float2 *part_ml;
+    int *arrived;
 };
 
 static bool aligned(const void *p, unsigned n) { return (((uintptr_t)p) & (n - 1)) == 0; }
@@ -49,6 +50,7 @@ static bool plan_cache(const aj_cache_config &cfg, aj_cache *h)
     const int64_t most = (int64_t)1 << 46;      // elements; offsets stay within 64 bits
     for (const int64_t s : {c.page_stride, c.slot_stride, c.head_stride})
         if (s < c.head_dim || s > most || s * h->kv_es % 16) return false;
+    if (c.slot_stride * h->kv_es * c.page_size >= (1LL << 32)) return false;
     if ((double)c.n_pages * c.page_stride + (double)c.page_size * c.slot_stride + (double)c.n_kv * c.head_stride > 1e18) return false;
     if (c.qkv_stride && (c.qkv_stride < row_q || c.qkv_stride > most || c.qkv_stride * h->es % 16)) return false;
     if (!c.q_stride) c.q_stride = row_q;
@@ -60,6 +62,7 @@ static void free_cache(aj_cache *h)
 {
     if (h->part_o) (void)hipFree(h->part_o);
     if (h->part_ml) (void)hipFree(h->part_ml);
+    if (h->arrived) (void)hipFree(h->arrived);
     delete h;
 }
 
@@ -88,14 +91,22 @@ extern "C" int aj_cache_create(const aj_cache_config *cfg, aj_cache **out)
     }
     if (c.B > 0) {
         const int vectors = (c.K + 1) * (c.n_q / c.n_kv);
-        h->plan = h->type == CACHE_F32   ? cache_attend_plan_f32(c.head_dim, vectors, cus)
-                  : h->type == CACHE_FP8 ? cache_attend_plan_fp8(c.head_dim, vectors, cus)
-                                         : cache_attend_plan_bf16(c.head_dim, vectors, cus);
-        const size_t units = (size_t)h->plan.clusters * 2 * h->plan.blocks * h->plan.vectors;
-        if (hipMalloc(&h->part_o, h->plan.part_floats * sizeof(float)) != hipSuccess || hipMalloc(&h->part_ml, units * sizeof(float2)) != hipSuccess) {
+        h->plan = h->type == CACHE_F32   ? cache_attend_plan_f32(c.head_dim, vectors, c.n_kv, cus)
+                  : h->type == CACHE_FP8 ? cache_attend_plan_fp8(c.head_dim, vectors, c.n_kv, cus)
+                                         : cache_attend_plan_bf16(c.head_dim, vectors, c.n_kv, cus);
+        const AttendPlan &p = h->plan;
+        const size_t counts = (size_t)p.clusters * p.heads * p.blocks * sizeof(int);
+        if (hipMalloc(&h->part_o, p.parts * p.part_size * sizeof(float)) != hipSuccess || hipMalloc(&h->part_ml, p.parts * sizeof(float2)) != hipSuccess ||
+            hipMalloc(&h->arrived, counts) != hipSuccess) {
             (void)hipGetLastError();
             free_cache(h);
             return AJ_ENOMEM;
+        }
+        e = hipMemset(h->arrived, 0, counts);
+        if (e == hipSuccess) e = hipDeviceSynchronize();
+        if (e != hipSuccess) {
+            free_cache(h);
+            return hip_fail(e);
         }
     }
     *out = h;
@@ -218,11 +229,15 @@ extern "C" int aj_cache_attend(aj_cache *h, const void *q, const void *k_pool, c
     a.q_stride = c.q_stride;
     a.score_scale = score_scale;
     a.v_scale = v_scale;
+    const bool few = (c.K + 1) * (c.n_q / c.n_kv) <= 32;
     a.clusters = h->plan.clusters;
+    a.heads = h->plan.heads;
+    a.groups = c.n_kv / h->plan.heads;
     a.blocks = h->plan.blocks;
+    a.least = few ? 2 : 1;
     a.part_o = h->part_o;
     a.part_ml = h->part_ml;
-    const bool few = (c.K + 1) * (c.n_q / c.n_kv) <= 32;
+    a.arrived = h->arrived;
     hipStream_t s = (hipStream_t)stream;
     const hipError_t e = h->type == CACHE_F32 ? cache_attend_f32(few, a, s) : h->type == CACHE_FP8 ? cache_attend_fp8(few, a, s) : cache_attend_bf16(few, a, s);
     return e == hipSuccess ? AJ_OK : hip_fail(e);

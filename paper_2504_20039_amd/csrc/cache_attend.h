@@ -18,12 +18,14 @@
 // Work.  Lengths are known on the device only.  All (window, head of keys and values) items' tiles form one line, which is cut into equal pieces for
 // `clusters` clusters of NB workgroups (one per block of QB vectors; a cluster's workgroups run on one XCD and read the same tokens at the same
 // time).  Every workgroup finds its piece by a prefix sum over the windows.  Items cut by a piece's border leave partial results (maximum, sum,
-// unscaled O in fp32), which join_kernel adds in the order of the pieces, so that the same call gives the same bits.
+// unscaled O in fp32), which the last workgroup to arrive adds in the order of the pieces, so that the same call gives the same bits.
 #pragma once
 #include <math.h>
 
 #include "cache.h"
 #include "lds_pipeline.h"
+
+#define ALWAYS_INLINE __attribute__((always_inline))
 
 namespace aj {
 
@@ -46,7 +48,7 @@ struct Form {
     static constexpr int TILE = ST * RB, STAGE = 2 * TILE;                    // keys, then values
     static constexpr int NI = TILE / 1024 / WAVES;                            // load instructions of a wave for the keys of a tile (values: the same)
     static constexpr int NKB = KT / 32, DB = DP / 32, QREGS = TYPE == CACHE_F32 ? DP / 8 : DP / 16;
-    static constexpr int SEG = 2048;                                          // page numbers in LDS
+    static constexpr int SEG = 1024;                                          // pages in LDS
     static constexpr int MERGE = WK > 1 ? WAVES * DP * 32 * 4 : 0;            // bytes to add up the waves' parts
     static constexpr int LDS = NST * STAGE > MERGE ? NST * STAGE : MERGE;
     static_assert(TILE % (1024 * WAVES) == 0 && CPR <= 64 && 2 * NI * (NST - 1) < 64, "whole load instructions, vmcnt");
@@ -93,23 +95,65 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi)
 
 // V^T as the A operand of a product over 16 tokens: element d = 32 db + lane % 32 of the tokens 16 ks + 4 h + {0..3} and 16 ks + 8 + 4 h + {0..3}.
 // Sixteen lanes give the addresses of 4 (8) rows of 16 elements, in pieces of 8 bytes, and lane i of them gets column i
+template <class T>
+__device__ __forceinline__ T from_lds(uint32_t at)
+{
+    return *(const __attribute__((address_space(3))) T *)at;
+}
+
 template <class F>
-__device__ __forceinline__ bf16x8 values(const char *vt, int ks, int db, int lane)
+__device__ __forceinline__ uint32_t values_base(int lane)      // of ks = db = 0, from the first row of the wave's values
 {
     const int h = lane >> 5, part = lane >> 4 & 1, i = lane & 15;
     if constexpr (F::TYPE == CACHE_BF16) {
-        typedef __attribute__((address_space(3))) i16x4 *at;
-        const int row = 16 * ks + 4 * h + (i >> 2), chunk = (4 * db + 2 * part + (i >> 1 & 1)) ^ f_v<F>(row);
-        const char *p = vt + row * F::RB + chunk * 16 + (i & 1) * 8;
-        const i16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)p), y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p + 8 * F::RB));
+        const int row = 4 * h + (i >> 2);
+        return row * F::RB + ((2 * part + (i >> 1 & 1)) ^ f_v<F>(row)) * 16 + (i & 1) * 8;
+    } else {
+        const int j = i >> 1, row = 4 * h + (j & 3) + 8 * (j >> 2);
+        return row * F::RB + (part ^ f_v<F>(row)) * 16 + (i & 1) * 8;
+    }
+}
+
+template <class F>
+__device__ __forceinline__ bf16x8 values(uint32_t base, int ks, int db)
+{
+    // the chunk's number is changed by exclusive or, so that is how 32 db elements are added
+    const uint32_t at = (base ^ (32 * db * F::KES)) + 16 * ks * F::RB;
+    if constexpr (F::TYPE == CACHE_BF16) {
+        typedef __attribute__((address_space(3))) i16x4 *p;
+        const i16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)at), y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)(at + 8 * F::RB));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-        typedef __attribute__((address_space(3))) i32x2 *at;
-        const int j = i >> 1, row = 16 * ks + 4 * h + (j & 3) + 8 * (j >> 2), chunk = (2 * db + part) ^ f_v<F>(row);
-        const i32x2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((at)(vt + row * F::RB + chunk * 16 + (i & 1) * 8));
+        typedef __attribute__((address_space(3))) i32x2 *p;
+        const i32x2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((p)at);
         return widen(y[0], y[1]);
     }
 }
+
+// Partial results go from one workgroup to another that may run on another XCD, behind another L2: stores and loads of the device's scope pass them by,
+// so that neither side has to write back or invalidate a cache (fences of that scope do both: 243 us instead of 198 for 64 windows of 17 .. 8192 tokens and 8 heads)
+struct Part {
+    static constexpr int DEVICE = 16;      // cache policy: sc1
+    __amdgpu_buffer_rsrc_t o, ml;
+
+    __device__ __forceinline__ Part(const AttendArgs &a, int64_t unit, int vectors, int size)
+        : o(__builtin_amdgcn_make_buffer_rsrc(a.part_o + unit * vectors * size, 0, vectors * size * 4, 0x00020000)),
+          ml(__builtin_amdgcn_make_buffer_rsrc(a.part_ml + unit * vectors, 0, vectors * 8, 0x00020000))
+    {
+    }
+    __device__ __forceinline__ void store(int at, f32x4 y) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), o, at * 16, 0, DEVICE); }
+    __device__ __forceinline__ void store(int x, float m, float l) const
+    {
+        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(m), __float_as_uint(l)}, ml, x * 8, 0, DEVICE);
+    }
+    __device__ __forceinline__ f32x4 load(int at) const { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(o, at * 16, 0, DEVICE)); }
+    __device__ __forceinline__ float2 load_ml(int x) const
+    {
+        const auto y = __builtin_amdgcn_raw_buffer_load_b64(ml, x * 8, 0, DEVICE);
+        return float2{__uint_as_float(y[0]), __uint_as_float(y[1])};
+    }
+};
 
 // Keeps what is computed from x where it is written: what is needed once per tile or per item would otherwise be computed ahead of the loops and take
 // registers throughout
@@ -117,6 +161,20 @@ __device__ __forceinline__ int here(int x)
 {
     asm volatile("" : "+v"(x));
     return x;
+}
+
+// Values that are the same in all lanes but are computed in vector registers (divisions, fp64).  (The compiler drops a readfirstlane of what it knows to
+// be the same in all lanes, and then has no scalar register for an operand that needs one)
+__device__ __forceinline__ int uniform(int x)
+{
+    asm("" : "+v"(x));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+__device__ __forceinline__ const char *uniform(const char *p)
+{
+    const uint64_t x = (uint64_t)p;
+    return (const char *)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
 // What a window's tokens look like to its rows
@@ -168,14 +226,14 @@ struct Line {
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) n += sums[w];
         __syncthreads();
-        return n * a.n_kv;
+        return n * a.groups;
     }
 
     __device__ __forceinline__ void find(const AttendArgs &a, int w, int &b_out, int &start_out) const
     {
         int *found = sums + THREADS / 64, carry = 0;
         for (int base = 0; base < a.pages.B; base += THREADS) {
-            const int b = base + (int)threadIdx.x, mine = b < a.pages.B ? span_of<ST>(a, b).n * a.n_kv : 0;
+            const int b = base + (int)threadIdx.x, mine = b < a.pages.B ? span_of<ST>(a, b).n * a.groups : 0;
             int incl = mine;
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
@@ -198,8 +256,8 @@ struct Line {
             __syncthreads();
             if (b_out >= 0) break;
         }
-        b_out = __builtin_amdgcn_readfirstlane(b_out);
-        start_out = __builtin_amdgcn_readfirstlane(start_out);
+        b_out = uniform(b_out);
+        start_out = uniform(start_out);
     }
 };
 
@@ -216,6 +274,11 @@ __device__ __forceinline__ f32x4 four(const char *at)
         return f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
     }
 }
+
+// The line's `total` places are cut into `cuts` pieces that differ by one place at most: the first place of a piece, and the piece of a place.
+// (Products are below 2^46 and quotients below 2^15: in fp64 no quotient is rounded to a whole number that it does not reach.)
+__device__ __forceinline__ int cut(int piece, int total, int cuts) { return uniform((int)((double)piece * total / cuts)); }
+__device__ __forceinline__ int piece_of(int place, int total, int cuts) { return uniform((int)((((double)place + 1.0) * cuts - 1.0) / total)); }
 
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
@@ -241,13 +304,61 @@ __device__ __forceinline__ void finish_lse(const AttendArgs &a, int64_t vec, flo
     if (a.lse) a.lse[vec] = l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * 0.69314718f : -INFINITY;
 }
 
+// Parts of one vector, pieces d0, d0 + step, .. of them.  These are round trips to memory, and count by the number of loads in flight: PARTS x PIECES
+template <class F, int PARTS, int PIECES, class P>
+__device__ __forceinline__ void join(const AttendArgs &a, const P &part, int c0, int c1, int xl, int64_t vec, int d0, int step)
+{
+    float m = -INFINITY, l = 0.f;
+    f32x4 o[PIECES];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) o[p] = f32x4{0, 0, 0, 0};
+    for (int cl = c0; cl <= c1; cl += PARTS) {
+        float2 ml[PARTS];
+        f32x4 y[PARTS][PIECES];
+#pragma unroll
+        for (int j = 0; j < PARTS; ++j) {
+            const Part one = part(cl + j < c1 ? cl + j : c1);      // (the last part once more counts for nothing)
+            ml[j] = one.load_ml(xl);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) y[j][p] = one.load((d0 + p * step < F::DP / 4 ? d0 + p * step : 0) * F::QB + xl);
+        }
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < PARTS; ++j)
+            top = fmaxf(top, ml[j].x);
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= keep;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) o[p] *= keep;
+#pragma unroll
+        for (int j = 0; j < PARTS; ++j) {
+            const float f = ml[j].x == -INFINITY || cl + j > c1 ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - m);
+            l += ml[j].y * f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) o[p] += y[j][p] * f;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+        if (d0 + p * step < a.D / 4) finish<F::TYPE>(a, vec, d0 + p * step, o[p], l);
+    if (d0 == 0) finish_lse(a, vec, m, l);
+}
+
+// Pages of a segment of an item's tiles, in LDS: byte offsets into a pool (page 0's for a page that is nowhere) and whether they are somewhere
+template <class F>
+struct Segment {
+    int64_t at[F::SEG];
+    uint8_t gone[F::SEG];
+};
+
 template <class F>
 __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PER_CU *F::WAVES / 4) void attend_kernel(AttendArgs a)
 {
-    constexpr int ST = F::ST, RB = F::RB, KT = F::KT, DB = F::DB, NKB = F::NKB, NI = F::NI, QB = F::QB;
+    constexpr int ST = F::ST, RB = F::RB, KT = F::KT, DB = F::DB, NKB = F::NKB, NI = F::NI, QB = F::QB, NST = F::NST;
     constexpr bool F32 = F::TYPE == CACHE_F32;
     __shared__ __attribute__((aligned(1024))) char lds[F::LDS];
-    __shared__ int tab[F::SEG];
+    __shared__ Segment<F> pages;
     __shared__ int sums[F::WAVES + 3];
     __shared__ int wflag[2][F::WAVES];
     __shared__ float mls[2][F::WK][QB];
@@ -259,11 +370,13 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 
     // this workgroup's piece of the line of tiles; its block of vectors
     const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, per_xcd = a.clusters / 8;
-    const int cluster = xcd * per_xcd + place / a.blocks, block = place % a.blocks;
+    const int members = a.heads * a.blocks, cluster = uniform(xcd * per_xcd + place / members), member = uniform(place % members);
+    const int block = uniform(member % a.blocks), head_of_group = uniform(member / a.blocks);
     const Line<ST, F::THREADS> line{sums};
-    const int total = line.total(a), chunk = (total + a.clusters - 1) / a.clusters;
-    int w = cluster * chunk;
-    const int w_end = w + chunk < total ? w + chunk : total;
+    const int total = uniform(line.total(a)), most = uniform(total / a.least), cuts = most < 1 ? 1 : most < a.clusters ? most : a.clusters;
+    if (cluster >= cuts) return;
+    int w = cut(cluster, total, cuts);
+    const int w_end = cut(cluster + 1, total, cuts);
     if (w >= w_end) return;
     int b, start;
     line.find(a, w, b, start);
@@ -271,16 +384,30 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 
     const uint32_t lds0 = lds_offset_of(lds);
     const float c = a.score_scale, threshold = 8.f / c;
+    const int per_tile = page < ST ? ST >> a.pages.log_page : 1, seg_tiles = F::SEG / per_tile;
+    const bool once = a.blocks == 1;
+    const uint32_t slot_stride = (uint32_t)a.pages.slot_stride;
+    // what a lane asks for in the n-th load instruction of a tile, behind the address of its page
+    uint32_t k_off[NI], v_off[NI];
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+        const int row = (wave * NI + n) * F::RPI + lane / F::CPR, pc = lane % F::CPR;
+        int ck = pc ^ f_k<F>(row), cv = pc ^ f_v<F>(row);
+        if (ck * 16 >= a.D * F::KES) ck = 0;      // padding: the query is zero there, and what comes of the values is not written
+        if (cv * 16 >= a.D * F::KES) cv = 0;
+        k_off[n] = (uint32_t)(row & (page - 1)) * slot_stride + ck * 16;
+        v_off[n] = (uint32_t)(row & (page - 1)) * slot_stride + cv * 16;
+    }
 
     while (w < w_end) {
-        while (w >= start + sp.n * a.n_kv) {      // (windows without rows have no places)
-            start += sp.n * a.n_kv;
+        while (w >= start + sp.n * a.groups) {      // (windows without rows have no places)
+            start += sp.n * a.groups;
             ++b;
             sp = span_of<ST>(a, b);
         }
-        const int kvh = (w - start) / sp.n, i_first = (w - start) % sp.n;
+        const int group = uniform((w - start) / sp.n), kvh = group * a.heads + head_of_group, i_first = w - start - group * sp.n;
         const int i_last = sp.n - i_first < w_end - w ? sp.n : i_first + (w_end - w);     // end of the visits
-        const int item = start + kvh * sp.n;                                              // first place of the item
+        const int item = start + group * sp.n;                                            // first place of the item
         const bool whole = i_first == 0 && i_last == sp.n;
         w += i_last - i_first;
         const int nvec = sp.R * G;
@@ -288,44 +415,52 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
         const int x_last = (block + 1) * QB < nvec ? (block + 1) * QB - 1 : nvec - 1;
         const int r_first = block * QB / G, r_last = x_last / G;
 
-        // the visits that this block needs: not those behind its last row, nor those before its first row's window
-        int i_begin = i_first, i_end = i_last;
+        // the visits that this block needs: not those behind its last row, nor those before its first row's window; among them, from i_full to i_part, the
+        // tiles of which every row of the block sees everything
+        int i_begin = i_first, i_end = i_last, i_full, i_part;
         {
             const int hi = sp.L + r_last + 1 < cap ? sp.L + r_last + 1 : cap;
             const int tile = (hi - 1) / ST, last = tile >= sp.first ? sp.ns + tile - sp.first : tile < sp.ns ? tile : sp.ns - 1;
             if (i_end > last + 1) i_end = last + 1 > i_begin ? last + 1 : i_begin;
-            if (a.window && !a.pages.depth && i_begin >= sp.ns) {
+            i_full = i_begin;
+            if (a.window) {
                 const int lo = sp.L + r_first - a.window + 1, i = sp.ns + lo / ST - sp.first;
-                if (lo > 0 && i > i_begin) i_begin = i < i_end ? i : i_end;
+                if (!a.pages.depth && i_begin >= sp.ns && lo > 0 && i > i_begin) i_begin = i < i_end ? i : i_end;
+                const int near = sp.L + r_last - a.window + 1, f = near > 0 ? sp.ns + (near + ST - 1) / ST - sp.first : 0;
+                i_full = i_begin > sp.ns ? i_begin : sp.ns;
+                i_full = f > i_full ? f : i_full;
             }
+            const int seen = a.mask || a.pages.depth ? sp.L : sp.L + r_first + 1, until = sp.ns + (seen < sp.hi ? seen : sp.hi) / ST - sp.first;
+            i_full = i_full < i_end ? i_full : i_end;
+            i_part = until < i_end ? until : i_end;
+            i_part = i_part > i_full ? i_part : i_full;
         }
 
         // queries as the B operand: column = vector
-        const int x = block * QB + wq * 32 + col, xc = x < nvec ? x : nvec - 1, r = xc / G, row_of_lane = r, head = kvh * G + xc % G;
+        const int x = block * QB + wq * 32 + col, xc = x < nvec ? x : nvec - 1, r = xc / G, head = kvh * G + xc % G;
         const bool active = block * QB + wq * 32 < nvec;
         const int64_t vec = ((int64_t)b * a.pages.rows + r) * a.n_q + head;
         u32x4 q[F::QREGS];
         {
             const char *row = (const char *)a.q + (((int64_t)b * a.pages.rows + r) * a.q_stride + head * a.D) * (F32 ? 4 : 2);
+            const int h = here(lane) >> 5;
 #pragma unroll
             for (int s = 0; s < F::QREGS; ++s) {
                 const int d = F32 ? 4 * (2 * s + h) : F::TYPE == CACHE_FP8 ? 16 * (2 * (s / 2) + h) + 8 * (s & 1) : 16 * s + 8 * h;
                 q[s] = d < a.D ? *(const u32x4 *)(row + d * (F32 ? 4 : 2)) : u32x4{0, 0, 0, 0};
             }
         }
-        const int my_depth = depth_of(a.pages, b, r);
+        int my_depth = depth_of(a.pages, b, r);
         f32x16 acc[DB];
 #pragma unroll
         for (int i = 0; i < DB; ++i) acc[i] = f32x16{0};
         float m = -INFINITY, l = 0.f;
 
-        const char *k_head = (const char *)a.k_pool + kvh * a.pages.head_stride, *v_head = (const char *)a.v_pool + kvh * a.pages.head_stride;
-        const int per_tile = page < ST ? ST >> a.pages.log_page : 1, seg_tiles = F::SEG / per_tile;
-        const auto tile_of_visit = [&](int i) { return i < sp.ns ? i : sp.first + i - sp.ns; };
+        const char *k_head = uniform((const char *)a.k_pool + kvh * a.pages.head_stride), *v_head = uniform((const char *)a.v_pool + kvh * a.pages.head_stride);
+        const auto tile_of_visit = [&](int i) ALWAYS_INLINE { return i < sp.ns ? i : sp.first + i - sp.ns; };
 
         for (int seg = i_begin; seg < i_end; seg += seg_tiles) {
             const int seg_end = seg + seg_tiles < i_end ? seg + seg_tiles : i_end;
-            // the segment's page numbers; -1: nowhere
             __syncthreads();
             int bad = 0;
             for (int e = tid; e < (seg_end - seg) * per_tile; e += F::THREADS) {
@@ -335,248 +470,291 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     p = a.pages.table[(int64_t)b * a.pages.width + (t >> a.pages.log_page)];
                     if ((uint32_t)p >= (uint32_t)a.pages.n_pages) p = -1;
                 }
-                tab[e] = p;
+                pages.at[e] = p < 0 ? 0 : p * a.pages.page_stride;
+                pages.gone[e] = p < 0;
                 const int until = page < ST ? t + page : t + ST;
                 if (p < 0 && t < sp.hi && !(t >= a.sinks && until <= sp.lo)) bad = 1;
             }
             bad = __any(bad);
             if (lane == 0) wflag[1][wave] = bad;
+            // what was loaded so far has to be there before the tiles' loads begin: a wait for it later would wait for them too
+#pragma unroll
+            for (int s = 0; s < F::QREGS; ++s) asm volatile("" : "+v"(q[s]));
+            asm volatile("" : "+v"(my_depth));
             __syncthreads();
             bad = 0;
 #pragma unroll
             for (int v = 0; v < F::WAVES; ++v) bad |= wflag[1][v];
+            bad = uniform(bad);
 
-            const auto page_of = [&](int i, int row) { return tab[(i - seg) * per_tile + (page < ST ? row >> a.pages.log_page : 0)]; };
-            const auto issue = [&](int i, int stage) {
-                const int t0 = tile_of_visit(i) * ST, ln = here(lane), row0 = wave * NI * F::RPI + ln / F::CPR, pc = ln % F::CPR;
-                int64_t off[NI];
+            const auto page_of = [&](int i, int row) ALWAYS_INLINE { return (i - seg) * per_tile + (page < ST ? row >> a.pages.log_page : 0); };
+            // Loads of tile i.  (A token that is nowhere reads a slot of page 0, and one behind the last the slot where it would be.)
+            const auto issue = [&](int i, int stage) ALWAYS_INLINE {
+                const int t0 = tile_of_visit(i) * ST;
+                const uint32_t dst = (uint32_t)uniform(lds0 + stage * F::STAGE + wave * NI * 1024);
+                if (page >= F::RPI) {
+                    // the rows of a load instruction lie on one page, whose address is the same for all lanes: lane n looks up that of the n-th instruction
+                    const int64_t mine = pages.at[page_of(i, (wave * NI + (lane < NI ? lane : 0)) * F::RPI)] +
+                                         (page > ST ? (uint64_t)(uint32_t)(t0 & (page - 1)) * slot_stride : 0);
+                    const int lo = (int)mine, hi = (int)(mine >> 32);
 #pragma unroll
-                for (int n = 0; n < NI; ++n) {
-                    // a token that is nowhere reads slot 0 of page 0; so does one behind the last
-                    const int row = row0 + n * F::RPI, p = page_of(i, row), keep = (p >= 0) & (t0 + row < sp.hi) ? -1 : 0;
-                    off[n] = (p & keep) * a.pages.page_stride + ((t0 + row) & (page - 1) & keep) * a.pages.slot_stride;
-                }
+                    for (int n = 0; n < NI; ++n) {
+                        const int64_t at = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, n) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, n));
+                        if (once) {
+                            lds_dma_16_nt(k_head + at, k_off[n], dst + n * 1024);
+                            lds_dma_16_nt(v_head + at, v_off[n], dst + n * 1024 + F::TILE);
+                        } else {
+                            lds_dma_16(k_head + at, k_off[n], dst + n * 1024);
+                            lds_dma_16(v_head + at, v_off[n], dst + n * 1024 + F::TILE);
+                        }
+                    }
+                } else {
+                    const int row0 = wave * NI * F::RPI + here(lane) / F::CPR;
+                    int64_t at[NI];
 #pragma unroll
-                for (int n = 0; n < NI; ++n) {
-                    const int row = row0 + n * F::RPI;
-                    int ck = pc ^ f_k<F>(row), cv = pc ^ f_v<F>(row);
-                    ck = ck * 16 >= a.D * F::KES ? 0 : ck;      // padding: the query is zero there, and so is what is written
-                    cv = cv * 16 >= a.D * F::KES ? 0 : cv;
-                    const uint32_t dst = lds0 + stage * F::STAGE + (wave * NI + n) * 1024;
-                    load_to_lds_16_at(k_head + off[n] + ck * 16, dst);
-                    load_to_lds_16_at(v_head + off[n] + cv * 16, dst + F::TILE);
+                    for (int n = 0; n < NI; ++n) at[n] = pages.at[page_of(i, row0 + n * F::RPI)];
+#pragma unroll
+                    for (int n = 0; n < NI; ++n) {
+                        load_to_lds_16_at(k_head + (at[n] + (uint32_t)here(k_off[n])), dst + n * 1024);
+                        load_to_lds_16_at(v_head + (at[n] + (uint32_t)here(v_off[n])), dst + n * 1024 + F::TILE);
+                    }
                 }
             };
 
+            // scores of the wave's tokens
+            f32x16 s[NKB];
+            const auto score = [&](uint32_t kt) ALWAYS_INLINE {
+                const uint32_t base = kt + here(col * RB + (h ^ f_k<F>(col)) * 16);
 #pragma unroll
-            for (int s = 0; s < F::NST - 1; ++s)
-                if (seg + s < seg_end) issue(seg + s, s);
-            int stage = 0;
-            for (int i = seg; i < seg_end; ++i) {
-                // tile i has landed, for every wave, and nobody reads the stage before it any more
-                if (F::NST > 3 && i + 2 < seg_end) wait_vm_lgkm_and_barrier<(F::NST > 3 ? 4 * NI : 0)>();
-                else if (F::NST > 2 && i + 1 < seg_end) wait_vm_lgkm_and_barrier<(F::NST > 2 ? 2 * NI : 0)>();
-                else wait_vm_lgkm_and_barrier<0>();
-                if (i + F::NST - 1 < seg_end) issue(i + F::NST - 1, stage == 0 ? F::NST - 1 : stage - 1);
-
-                const int t_tile = tile_of_visit(i) * ST;
-                const bool full = !bad && t_tile + ST <= sp.L && t_tile + ST <= sp.hi &&
-                                  (!a.window || t_tile + ST <= a.sinks || sp.L + r_last - t_tile < a.window);
-                char *tile = lds + stage * F::STAGE;
-                bool poisoned = false;
-                if (!full) {
-                    // values of tokens that nobody sees count as zero whatever they are; and look for values that are not finite
-                    int odd = 0;
-                    for (int e = here(tid); e < ST * F::CPR; e += F::THREADS) {
-                        const int row = e / F::CPR, t = t_tile + row;
-                        const bool dead = t >= sp.hi || (a.window && t >= a.sinks && t < sp.lo) || page_of(i, row) < 0;
-                        u32x4 *at = (u32x4 *)(tile + F::TILE + e * 16);
-                        if (dead) *at = u32x4{0, 0, 0, 0};
-                        else if (sp.R > 1) {
-                            const u32x4 y = *at;
+                for (int kb = 0; kb < NKB; ++kb) s[kb] = f32x16{0};
+                // fragments are asked for two steps ahead; the barriers keep the compiler from asking for all of them at once, which
+                // would take more registers than there are
+                constexpr int KS = RB / 32, AHEAD = 2;
+                u32x4 y[AHEAD + 1][NKB];
+                const auto ask = [&](int ks) ALWAYS_INLINE {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                if constexpr (F32) odd |= (y[j] & 0x7f800000u) == 0x7f800000u;
-                                else if constexpr (F::TYPE == CACHE_BF16) odd |= (y[j] & 0x7f80u) == 0x7f80u || (y[j] & 0x7f800000u) == 0x7f800000u;
-                                else odd |= (((y[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
-                            }
+                    for (int kb = 0; kb < NKB; ++kb) y[ks % (AHEAD + 1)][kb] = from_lds<u32x4>((base ^ (32 * ks)) + kb * 32 * RB);
+                };
+#pragma unroll
+                for (int ks = 0; ks < AHEAD && ks < KS; ++ks) ask(ks);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    if (ks + AHEAD < KS) ask(ks + AHEAD);
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb) {
+                        const u32x4 z = y[ks % (AHEAD + 1)][kb];
+                        if constexpr (F32) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(z[e]), __uint_as_float(q[ks][e]), s[kb], 0, 0, 0);
+                        } else if constexpr (F::TYPE == CACHE_BF16) {
+                            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), __builtin_bit_cast(bf16x8, q[ks]), s[kb], 0, 0, 0);
+                        } else {
+                            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(z[0], z[1]), __builtin_bit_cast(bf16x8, q[2 * ks]), s[kb], 0, 0, 0);
+                            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(z[2], z[3]), __builtin_bit_cast(bf16x8, q[2 * ks + 1]), s[kb], 0, 0, 0);
                         }
                     }
-                    odd = __any(odd);
-                    if (lane == 0) wflag[0][wave] = odd;
-                    __syncthreads();
-#pragma unroll
-                    for (int v = 0; v < F::WAVES; ++v) poisoned |= wflag[0][v] != 0;
-                }
-
-                if (active) {
-                    const char *kt = tile + wk * KT * RB, *vt = tile + F::TILE + wk * KT * RB;
-                    const int t0 = t_tile + wk * KT;
-                    f32x16 s[NKB];
-#pragma unroll
-                    for (int kb = 0; kb < NKB; ++kb) s[kb] = f32x16{0};
-                    // fragments are asked for two steps ahead; the barriers keep the compiler from asking for all of them at once, which
-                    // would take more registers than there are
-                    constexpr int KS = RB / 32, AHEAD = 2;
-                    u32x4 y[AHEAD + 1][NKB];
-                    const auto ask = [&](int ks) {
-#pragma unroll
-                        for (int kb = 0; kb < NKB; ++kb) y[ks % (AHEAD + 1)][kb] = *(const u32x4 *)(kt + (kb * 32 + col) * RB + (((2 * ks + h) ^ f_k<F>(col)) * 16));
-                    };
-#pragma unroll
-                    for (int ks = 0; ks < AHEAD && ks < KS; ++ks) ask(ks);
                     __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            // scores to weights
+            const auto weigh = [&]() ALWAYS_INLINE {
+                float mx = -INFINITY;
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        if (ks + AHEAD < KS) ask(ks + AHEAD);
+                for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                        for (int kb = 0; kb < NKB; ++kb) {
-                            const u32x4 z = y[ks % (AHEAD + 1)][kb];
-                            if constexpr (F32) {
+                    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+                mx = max_halves(mx);
+                if (__any(mx > m + threshold)) {
+                    const float mn = fmaxf(m, mx), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(z[e]), __uint_as_float(q[ks][e]), s[kb], 0, 0, 0);
-                            } else if constexpr (F::TYPE == CACHE_BF16) {
-                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), __builtin_bit_cast(bf16x8, q[ks]), s[kb], 0, 0, 0);
-                            } else {
-                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(z[0], z[1]), __builtin_bit_cast(bf16x8, q[2 * ks]), s[kb], 0, 0, 0);
-                                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(z[2], z[3]), __builtin_bit_cast(bf16x8, q[2 * ks + 1]), s[kb], 0, 0, 0);
-                            }
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
+                    for (int i = 0; i < DB; ++i)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[i][e] *= f;
+                    l *= f;
+                    m = mn;
+                }
+                const float base = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c, -base));
+                        l += s[kb][e];
                     }
-
-                    uint32_t vis[NKB];
-                    if (!full) {
-#pragma unroll
-                        for (int kb = 0; kb < NKB; ++kb) {
-                            const int t = t0 + 32 * kb, r = here(row_of_lane);
-                            uint32_t y = below(sp.hi - t) & below(sp.L + r + 1 - t);
-                            const uint32_t old = below(sp.L - t);
-                            if (a.mask && old != ~0u) {
-                                const uint32_t *mw = a.mask + ((int64_t)b * a.pages.rows + r) * words;
-                                const int at = t - sp.L, wd = at >> 5, sh = at & 31;      // (at > -32)
-                                const uint32_t m0 = wd >= 0 && wd < words ? mw[wd] : 0u, m1 = wd + 1 < words ? mw[wd + 1] : 0u;
-                                y &= old | (sh ? m0 >> sh | m1 << (32 - sh) : m0);
-                            }
-                            if (a.window) {
-                                const uint32_t sunk = below(a.sinks - t), near = ~below(sp.L + my_depth - a.window + 1 - t);
-                                if (!a.pages.depth) {
-                                    y &= sunk | near;
-                                } else {
-                                    y &= ~old | sunk | near;
-                                    if (my_depth >= a.window)      // new rows further away than the window
-                                        for (uint32_t left = y & ~old; left; left &= left - 1) {
-                                            const int e = __ffs(left) - 1, d = depth_of(a.pages, b, t + e - sp.L);
-                                            if (my_depth - d >= a.window && sp.L + d >= a.sinks) y &= ~(1u << e);
-                                        }
-                                }
-                            }
-                            if (bad)
-                                for (int e = 0; e < 32; ++e)
-                                    if (page_of(i, wk * KT + kb * 32 + e) < 0) y &= ~(1u << e);
-                            vis[kb] = y;
-                            y >>= 4 * h;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                s[kb][e] = y >> (e % 4 + 8 * (e / 4)) & 1 ? s[kb][e] : -INFINITY;
-                        }
-                    }
-
-                    float mx = -INFINITY;
+                }
+            };
+            // O^T += V^T P^T
+            const auto add = [&](uint32_t vt) ALWAYS_INLINE {
+                if constexpr (F32) {
+                    const uint32_t base = vt + here(4 * h * RB + ((col >> 2) ^ (h << 3)) * 16 + (col & 3) * 4);
 #pragma unroll
                     for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-                    mx = max_halves(mx);
-                    if (__any(mx > m + threshold)) {
-                        const float mn = fmaxf(m, mx), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
-#pragma unroll
-                        for (int i = 0; i < DB; ++i)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) acc[i][e] *= f;
-                        l *= f;
-                        m = mn;
-                    }
-                    const float base = m == -INFINITY ? 0.f : m * c;
-#pragma unroll
-                    for (int kb = 0; kb < NKB; ++kb) {
-#pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c, -base));
-                            l += s[kb][e];
-                        }
-                    }
-
-                    // O^T += V^T P^T
-                    if (poisoned) {
-                        // some values are not finite: a token at a time, and only for the vectors that see it
-                        for (int e = 0; e < KT; ++e) {
-                            const int h = here(lane) >> 5;
-                            const int from = e % 32 % 4 + 4 * (e % 32 / 8);      // the register and (below) the half that have its weight
-                            float p = 0.f;
-                            uint32_t seen = 0;
-#pragma unroll
-                            for (int kb = 0; kb < NKB; ++kb) {
-                                if (kb == e / 32) seen = vis[kb] >> (e % 32) & 1;
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) p = kb == e / 32 && j == from ? s[kb][j] : p;
-                            }
-                            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(p), __float_as_uint(p), false, false);
-                            p = __uint_as_float(e >> 2 & 1 ? both[1] : both[0]);
-                            const char *row = vt + e * RB;
-                            const int f = f_v<F>(wk * KT + e);
+                            float y[DB];
 #pragma unroll
                             for (int db = 0; db < DB; ++db)
+                                y[db] = from_lds<float>((base ^ (128 * db)) + (kb * 32 + e % 4 + 8 * (e / 4)) * RB);
 #pragma unroll
-                                for (int g = 0; g < 4; ++g) {
-                                    const int at = (32 * db + 8 * g + 4 * h) * F::KES;
-                                    const f32x4 y = four<F>(row + ((at / 16) ^ f) * 16 + at % 16);
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j) acc[db][4 * g + j] = seen ? fmaf(p, y[j], acc[db][4 * g + j]) : acc[db][4 * g + j];
-                                }
+                            for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[db], s[kb][e], acc[db], 0, 0, 0);
                         }
-                    } else if constexpr (F32) {
+                } else {
+                    constexpr int KS = KT / 16;
+                    const uint32_t base = vt + values_base<F>(here(lane));
+                    bf16x8 y[2][DB];
 #pragma unroll
-                        for (int kb = 0; kb < NKB; ++kb)
+                    for (int db = 0; db < DB; ++db) y[0][db] = values<F>(base, 0, db);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                float y[DB];
+                    for (int ks = 0; ks < KS; ++ks) {
+                        bf16x8 p;      // weights lose at most half a step of bf16, 2^-8 of each: as the products' operand they have to
 #pragma unroll
-                                for (int db = 0; db < DB; ++db)
-                                    y[db] = *(const float *)(vt + (kb * 32 + e % 4 + 8 * (e / 4) + 4 * h) * RB + (((8 * db + (col >> 2)) ^ (h << 3)) * 16) + (col & 3) * 4);
+                        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[ks / 2][8 * (ks & 1) + e];
+                        if (ks + 1 < KS) {
 #pragma unroll
-                                for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[db], s[kb][e], acc[db], 0, 0, 0);
-                            }
-                    } else {
-                        constexpr int KS = KT / 16;
-                        bf16x8 y[2][DB];
+                            for (int db = 0; db < DB; ++db) y[(ks + 1) & 1][db] = values<F>(base, ks + 1, db);
+                        }
 #pragma unroll
-                        for (int db = 0; db < DB; ++db) y[0][db] = values<F>(vt, 0, db, lane);
+                        for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[ks & 1][db], p, acc[db], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            };
+
+            // first the tiles that are seen whole, then the others: their loads form one sequence
+            int f0 = i_full > seg ? i_full : seg, f1 = i_part < seg_end ? i_part : seg_end;
+            if (f0 > seg_end) f0 = seg_end;
+            if (f1 < f0 || bad) f1 = f0;
+            const int nf = f1 - f0, n_all = seg_end - seg;
+            const auto visit = [&](int n) ALWAYS_INLINE { return n < nf ? f0 + n : n - nf < f0 - seg ? seg + n - nf : n - nf + seg + nf; };
 #pragma unroll
-                        for (int ks = 0; ks < KS; ++ks) {
-                            bf16x8 p;      // weights lose at most half a step of bf16, 2^-8 of each: as the products' operand they have to
+            for (int n = 0; n < NST - 1; ++n)
+                if (n < n_all) issue(visit(n), n);
+            int stage = 0;
+            const auto next = [&](int n) ALWAYS_INLINE {
+                // tile n has landed, for every wave, and nobody reads the stage before it any more
+                if (NST > 3 && n + 2 < n_all) wait_vm_lgkm_and_barrier<(NST > 3 ? 4 * NI : 0)>();
+                else if (NST > 2 && n + 1 < n_all) wait_vm_lgkm_and_barrier<(NST > 2 ? 2 * NI : 0)>();
+                else wait_vm_lgkm_and_barrier<0>();
+                if (n + NST - 1 < n_all) issue(visit(n + NST - 1), stage == 0 ? NST - 1 : stage - 1);
+            };
+            for (int n = 0; n < nf; ++n) {
+                next(n);
+                if (active) {
+                    const uint32_t tile = lds0 + stage * F::STAGE + wk * KT * RB;
+                    score(tile);
+                    weigh();
+                    add(tile + F::TILE);
+                }
+                stage = stage + 1 == NST ? 0 : stage + 1;
+            }
+
+            for (int n = nf; n < n_all; ++n) {
+                next(n);
+                const int i = visit(n), t_tile = tile_of_visit(i) * ST;
+                char *tile = lds + stage * F::STAGE;
+                stage = stage + 1 == NST ? 0 : stage + 1;
+                // values of tokens that nobody sees count as zero whatever they are; and look for values that are not finite
+                int odd = 0;
+                for (int e = here(tid); e < ST * F::CPR; e += F::THREADS) {
+                    const int row = e / F::CPR, t = t_tile + row;
+                    const bool dead = t >= sp.hi || (a.window && t >= a.sinks && t < sp.lo) || pages.gone[page_of(i, row)];
+                    u32x4 *at = (u32x4 *)(tile + F::TILE + e * 16);
+                    if (dead) *at = u32x4{0, 0, 0, 0};
+                    else if (sp.R > 1) {
+                        const u32x4 y = *at;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[ks / 2][8 * (ks & 1) + e];
-                            if (ks + 1 < KS) {
-#pragma unroll
-                                for (int db = 0; db < DB; ++db) y[(ks + 1) & 1][db] = values<F>(vt, ks + 1, db, lane);
-                            }
-#pragma unroll
-                            for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[ks & 1][db], p, acc[db], 0, 0, 0);
-                            __builtin_amdgcn_sched_barrier(0);
+                        for (int j = 0; j < 4; ++j) {
+                            if constexpr (F32) odd |= (y[j] & 0x7f800000u) == 0x7f800000u;
+                            else if constexpr (F::TYPE == CACHE_BF16) odd |= (y[j] & 0x7f80u) == 0x7f80u || (y[j] & 0x7f800000u) == 0x7f800000u;
+                            else odd |= (((y[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
                         }
                     }
                 }
-                stage = stage + 1 == F::NST ? 0 : stage + 1;
+                odd = __any(odd);
+                if (lane == 0) wflag[0][wave] = odd;
+                __syncthreads();
+                odd = 0;
+#pragma unroll
+                for (int v = 0; v < F::WAVES; ++v) odd |= wflag[0][v];
+                if (!active) continue;
+
+                const char *vt = tile + F::TILE + wk * KT * RB;
+                score(lds_offset_of(tile) + wk * KT * RB);
+                uint32_t vis[NKB];      // bit e: the lane's row sees token e of the 32
+                const int r = (block * QB + wq * 32 + (here(lane) & 31) < nvec ? block * QB + wq * 32 + (here(lane) & 31) : nvec - 1) / G;
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb) {
+                    const int t = t_tile + wk * KT + 32 * kb;
+                    uint32_t y = below(sp.hi - t) & below(sp.L + r + 1 - t);
+                    const uint32_t old = below(sp.L - t);
+                    if (a.mask && old != ~0u) {
+                        const uint32_t *mw = a.mask + ((int64_t)b * a.pages.rows + r) * words;
+                        const int at = t - sp.L, wd = at >> 5, sh = at & 31;      // (at > -32)
+                        const uint32_t m0 = wd >= 0 && wd < words ? mw[wd] : 0u, m1 = wd + 1 < words ? mw[wd + 1] : 0u;
+                        y &= old | (sh ? m0 >> sh | m1 << (32 - sh) : m0);
+                    }
+                    if (a.window) {
+                        const uint32_t sunk = below(a.sinks - t), near = ~below(sp.L + my_depth - a.window + 1 - t);
+                        if (!a.pages.depth) {
+                            y &= sunk | near;
+                        } else {
+                            y &= ~old | sunk | near;
+                            if (my_depth >= a.window)      // new rows further away than the window
+                                for (uint32_t left = y & ~old; left; left &= left - 1) {
+                                    const int e = __ffs(left) - 1, d = depth_of(a.pages, b, t + e - sp.L);
+                                    if (my_depth - d >= a.window && sp.L + d >= a.sinks) y &= ~(1u << e);
+                                }
+                        }
+                    }
+                    if (bad)
+                        for (int e = 0; e < 32; ++e)
+                            if (pages.gone[page_of(i, wk * KT + kb * 32 + e)]) y &= ~(1u << e);
+                    vis[kb] = y;
+                    y >>= 4 * (here(lane) >> 5);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[kb][e] = y >> (e % 4 + 8 * (e / 4)) & 1 ? s[kb][e] : -INFINITY;
+                }
+                weigh();
+                if (!odd) {
+                    add(lds_offset_of(vt));
+                    continue;
+                }
+                // some values are not finite: a token at a time, and only for the vectors that see it
+                for (int e = 0; e < KT; ++e) {
+                    const int h = here(lane) >> 5, from = e % 32 % 4 + 4 * (e % 32 / 8);      // the register and (below) the half that have its weight
+                    float p = 0.f;
+                    uint32_t seen = 0;
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb) {
+                        if (kb == e / 32) seen = vis[kb] >> (e % 32) & 1;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) p = kb == e / 32 && j == from ? s[kb][j] : p;
+                    }
+                    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(p), __float_as_uint(p), false, false);
+                    p = __uint_as_float(e >> 2 & 1 ? both[1] : both[0]);
+                    const char *row = vt + e * RB;
+                    const int f = f_v<F>(wk * KT + e);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const int at = (32 * db + 8 * g + 4 * h) * F::KES;
+                            const f32x4 y = four<F>(row + ((at / 16) ^ f) * 16 + at % 16);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) acc[db][4 * g + j] = seen ? fmaf(p, y[j], acc[db][4 * g + j]) : acc[db][4 * g + j];
+                        }
+                }
             }
         }
 
         // the halves' sums; the waves that shared the block's tokens
         l = sum_halves(l);
-        const int64_t unit = ((int64_t)cluster * 2 + (item > cluster * chunk)) * a.blocks + block;
-        float *part_o = a.part_o + unit * QB * F::DP;
-        float2 *part_ml = a.part_ml + unit * QB;
+        // (of a cluster's items, the first may have begun in an earlier one and the last may end in a later one)
+        const int c0 = piece_of(item, total, cuts), c1 = piece_of(item + sp.n - 1, total, cuts), later = item > cut(c0, total, cuts);
+        const auto unit = [&](int cl) ALWAYS_INLINE { return ((int64_t)cl * 2 + (cl == c0 ? later : 0)) * members + member; };
+        const Part mine_part(a, unit(cluster), QB, F::DP);
         if constexpr (F::WK == 1) {
             const int col = here(lane) & 31, h = here(lane) >> 5;
             if (x < nvec) {
@@ -587,11 +765,11 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                         const f32x4 o = {acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]};
                         const int d4 = 8 * db + 2 * e + h;
                         if (whole) finish<F::TYPE>(a, vec, d4, o, l);
-                        else *(f32x4 *)(part_o + ((int64_t)d4 * QB + wq * 32 + col) * 4) = o;
+                        else mine_part.store(d4 * QB + wq * 32 + col, o);
                     }
                 if (h == 0) {
                     if (whole) finish_lse(a, vec, m * c, l);
-                    else part_ml[wq * 32 + col] = float2{m * c, l};
+                    else mine_part.store(wq * 32 + col, m * c, l);
                 }
             }
         } else {
@@ -625,71 +803,62 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                 }
                 const int64_t vx = ((int64_t)b * a.pages.rows + xx / G) * a.n_q + kvh * G + xx % G;
                 if (whole) finish<F::TYPE>(a, vx, d4, o, tl);
-                else *(f32x4 *)(part_o + (int64_t)e * 4) = o;
+                else mine_part.store(e, o);
                 if (d4 == 0) {
                     if (whole) finish_lse(a, vx, tm * c, tl);
-                    else part_ml[xl] = float2{tm * c, tl};
+                    else mine_part.store(xl, tm * c, tl);
                 }
             }
             // (the barrier before the next item's page numbers keeps its loads out of `merge`)
         }
-    }
-}
+        if (whole) continue;
 
-// Adds the parts of the item that is cut at the border between clusters c and c + 1 for the first time, c = blockIdx.x
-template <class F>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a)
-{
-    constexpr int QB = F::QB, ND = 256 / QB;
-    __shared__ int sums[256 / 64 + 3];
-    const Line<F::ST, 256> line{sums};
-    const int total = line.total(a), chunk = (total + a.clusters - 1) / a.clusters;
-    const int border = ((int)blockIdx.x + 1) * chunk, block = blockIdx.y;
-    if (border >= total) return;
-    int b, start;
-    line.find(a, border, b, start);
-    const Span sp = span_of<F::ST>(a, b);
-    const int kvh = (border - start) / sp.n, item = start + kvh * sp.n;
-    if (item == border || item / chunk != (int)blockIdx.x) return;      // not cut here, or not for the first time
-    const int last = (item + sp.n - 1) / chunk;
-    const int G = a.n_q / a.n_kv, nvec = sp.R * G, xl = threadIdx.x % QB, x = block * QB + xl, d4 = blockIdx.z * ND + threadIdx.x / QB;
-    if (x >= nvec || 4 * d4 >= a.D) return;
-    const auto unit = [&](int c) { return ((int64_t)c * 2 + (item > c * chunk)) * a.blocks + block; };
-    float m = -INFINITY, l = 0.f;
-    for (int c = blockIdx.x; c <= last; ++c) m = fmaxf(m, a.part_ml[unit(c) * QB + xl].x);
-    f32x4 o = {0, 0, 0, 0};
-    for (int c = blockIdx.x; c <= last; ++c) {
-        const float2 ml = a.part_ml[unit(c) * QB + xl];
-        const f32x4 y = *(const f32x4 *)(a.part_o + (unit(c) * F::DP / 4 + d4) * QB * 4 + xl * 4);
-        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-        l += ml.y * f;
-        o += y * f;
+        // The workgroup that is the last of the item's to arrive adds the parts, in the order of the clusters whoever it is, and leaves the
+        // count at zero for the next call.  The border behind cluster c cuts one item at most
+        int *arrived = a.arrived + c0 * members + member;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the part is there
+        __syncthreads();
+        if (tid == 0) sums[0] = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (uniform(sums[0]) != c1 - c0) continue;      // (`sums` is next written behind another barrier)
+        if (tid == 0) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // a thread adds for one vector, as many pieces of 4 elements as it has to
+        const int nv = x_last + 1 - block * QB, log_nv = nv > 1 ? 32 - __builtin_clz(nv - 1) : 0;
+        const int xl = here(tid) & ((1 << log_nv) - 1), first = here(tid) >> log_nv, step = F::THREADS >> log_nv;
+        if (xl >= nv) continue;
+        const int xx = block * QB + xl;
+        const int64_t vx = ((int64_t)b * a.pages.rows + xx / G) * a.n_q + kvh * G + xx % G;
+        const auto part = [&](int cl) ALWAYS_INLINE { return Part(a, unit(cl), QB, F::DP); };
+        if (step >= a.D / 4) {
+            if (first < a.D / 4) join<F, 16, 1>(a, part, c0, c1, xl, vx, first, step);
+        } else {
+            for (int d0 = first; d0 < a.D / 4; d0 += 4 * step) join<F, 8, 4>(a, part, c0, c1, xl, vx, d0, step);
+        }
     }
-    const int64_t vec = ((int64_t)b * a.pages.rows + x / G) * a.n_q + kvh * G + x % G;
-    finish<F::TYPE>(a, vec, d4, o, l);
-    if (d4 == 0) finish_lse(a, vec, m, l);
 }
 
 template <class F>
 hipError_t launch_attend(const AttendArgs &a, hipStream_t s)
 {
-    attend_kernel<F><<<a.clusters * a.blocks, F::THREADS, 0, s>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    join_kernel<F><<<dim3(a.clusters - 1, a.blocks, F::DP / 4 / (256 / F::QB)), 256, 0, s>>>(a);
+    attend_kernel<F><<<a.clusters * a.heads * a.blocks, F::THREADS, 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <class F>
-AttendPlan plan_attend(int vectors, int num_cus)
+AttendPlan plan_attend(int vectors, int n_kv, int num_cus)
 {
     AttendPlan p;
     p.vectors = F::QB;
     p.tokens = F::ST;
     p.blocks = (vectors + F::QB - 1) / F::QB;
-    const int per_xcd = num_cus / 8 * F::PER_CU / p.blocks;
+    const int places = num_cus / 8 * F::PER_CU;      // of an XCD
+    p.heads = 1;
+    for (int h = 2; h <= n_kv; ++h)
+        if (n_kv % h == 0 && places / (h * p.blocks) * h * p.blocks * 10 >= places * 9) p.heads = h;
+    const int per_xcd = places / (p.heads * p.blocks);
     p.clusters = 8 * (per_xcd < 1 ? 1 : per_xcd);
-    p.part_floats = (size_t)p.clusters * 2 * p.blocks * F::QB * F::DP;
+    p.parts = (size_t)p.clusters * 2 * p.heads * p.blocks * F::QB;
+    p.part_size = F::DP;
     return p;
 }
 

@@ -4,7 +4,7 @@
 namespace aj {
 
 template <int DP, bool FEW> struct Choice;
-template <> struct Choice<64, true> { typedef Form<CACHE_F32, 64, 1, 4, 32, 2, 1> F; };
+template <> struct Choice<64, true> { typedef Form<CACHE_F32, 64, 1, 2, 32, 2, 2> F; };
 template <> struct Choice<128, true> { typedef Form<CACHE_F32, 128, 1, 2, 32, 2, 1> F; };
 template <> struct Choice<256, true> { typedef Form<CACHE_F32, 256, 4, 1, 32, 2, 1> F; };
 template <> struct Choice<64, false> { typedef Form<CACHE_F32, 64, 4, 1, 64, 2, 2> F; };
@@ -23,14 +23,14 @@ hipError_t cache_attend_f32(bool few, const AttendArgs &a, hipStream_t s)
 }
 
 template <int DP>
-static AttendPlan plan(int vectors, int num_cus)
+static AttendPlan plan(int vectors, int n_kv, int num_cus)
 {
-    return vectors <= 32 ? plan_attend<typename Choice<DP, true>::F>(vectors, num_cus) : plan_attend<typename Choice<DP, false>::F>(vectors, num_cus);
+    return vectors <= 32 ? plan_attend<typename Choice<DP, true>::F>(vectors, n_kv, num_cus) : plan_attend<typename Choice<DP, false>::F>(vectors, n_kv, num_cus);
 }
 
-AttendPlan cache_attend_plan_f32(int D, int vectors, int num_cus)
+AttendPlan cache_attend_plan_f32(int D, int vectors, int n_kv, int num_cus)
 {
-    return D <= 64 ? plan<64>(vectors, num_cus) : D <= 128 ? plan<128>(vectors, num_cus) : plan<256>(vectors, num_cus);
+    return D <= 64 ? plan<64>(vectors, n_kv, num_cus) : D <= 128 ? plan<128>(vectors, n_kv, num_cus) : plan<256>(vectors, n_kv, num_cus);
 }
 
 }  // namespace aj
