@@ -63,10 +63,10 @@ struct AttendArgs {
     const uint32_t *mask;
     void *out;
     float *lse;
-    int n_q, n_kv, D, window, sinks;
+    int n_q, n_kv, G, D, window, sinks;   // G = n_q / n_kv
     int64_t q_stride;      // elements
     float score_scale;     // scale * k_scale * log2(e): weights are powers of two
-    float v_scale;
+    float v_scale, inv_G;
     // the line of tiles is cut into `clusters` pieces; a cluster has a workgroup for each of `heads` heads of keys and values and `blocks` blocks of
     // vectors; groups = n_kv / heads.  Partial results of two items per piece
     int clusters, heads, groups, blocks;

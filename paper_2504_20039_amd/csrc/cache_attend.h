@@ -186,11 +186,11 @@ struct Span {
 };
 
 template <int ST>
-__device__ __forceinline__ Span span_of(const AttendArgs &a, int b)
+__device__ __forceinline__ Span span_of(const AttendArgs &a, int L, int R)
 {
     Span s;
-    s.L = cached_tokens(a.pages, b);
-    s.R = live_rows(a.pages, b);
+    s.L = L;
+    s.R = R;
     s.lo = s.ns = s.first = 0;
     const int cap = a.pages.width << a.pages.log_page;
     s.hi = s.L + s.R < cap ? s.L + s.R : cap;
@@ -209,55 +209,86 @@ __device__ __forceinline__ Span span_of(const AttendArgs &a, int b)
     return s;
 }
 
-// tiles of all items, and the window that has place w of their line: its number and its first place
+template <int ST>
+__device__ __forceinline__ Span span_of(const AttendArgs &a, int b)
+{
+    return span_of<ST>(a, cached_tokens(a.pages, b), live_rows(a.pages, b));
+}
+
+// The line's `total` places are cut into `cuts` pieces that differ by one place at most: the first place of a piece, and the piece of a place.
+// (Products are below 2^46 and quotients below 2^15: in fp64 no quotient is rounded to a whole number that it does not reach.)
+__device__ __forceinline__ int cut(int piece, int total, int cuts) { return uniform((int)((double)piece * total / cuts)); }
+__device__ __forceinline__ int piece_of(int place, int total, int cuts) { return uniform((int)((((double)place + 1.0) * cuts - 1.0) / total)); }
+
+// A workgroup's piece of the line of all items' tiles, and the window where it begins
 template <int ST, int THREADS>
 struct Line {
-    int *sums;   // LDS, THREADS / 64 + 3
+    int total, cuts, w, w_end;   // places of the line, pieces, the piece
+    int b, start, L, R;          // the window, its first place, its cached tokens and live rows
 
-    __device__ __forceinline__ int total(const AttendArgs &a) const
+    // sum of the values of the threads before this one and of all threads
+    static __device__ __forceinline__ void scan(int mine, int *sums, int &before, int &all)
     {
-        int n = 0;
-        for (int b = threadIdx.x; b < a.pages.B; b += THREADS) n += span_of<ST>(a, b).n;
+        int incl = mine;
 #pragma unroll
-        for (int o = 32; o; o /= 2) n += __shfl_xor(n, o);
-        if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = n;
+        for (int o = 1; o < 64; o *= 2) {
+            const int y = __shfl_up(incl, o);
+            if ((int)threadIdx.x % 64 >= o) incl += y;
+        }
+        if (threadIdx.x % 64 == 63) sums[threadIdx.x / 64] = incl;
         __syncthreads();
-        n = 0;
+        before = incl - mine;
+        all = 0;
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) n += sums[w];
-        __syncthreads();
-        return n * a.groups;
+        for (int v = 0; v < THREADS / 64; ++v) {
+            if (v < (int)threadIdx.x / 64) before += sums[v];
+            all += sums[v];
+        }
     }
 
-    __device__ __forceinline__ void find(const AttendArgs &a, int w, int &b_out, int &start_out) const
+    __device__ __forceinline__ bool begin(const AttendArgs &a, int cluster, int clusters, int *sums, int *found)
     {
-        int *found = sums + THREADS / 64, carry = 0;
-        for (int base = 0; base < a.pages.B; base += THREADS) {
-            const int b = base + (int)threadIdx.x, mine = b < a.pages.B ? span_of<ST>(a, b).n * a.groups : 0;
-            int incl = mine;
-#pragma unroll
-            for (int o = 1; o < 64; o *= 2) {
-                const int y = __shfl_up(incl, o);
-                if ((int)threadIdx.x % 64 >= o) incl += y;
+        const int B = a.pages.B, tid = threadIdx.x;
+        int mine = 0, before = 0, all = 0, my_L = 0, my_R = 0;      // (what differs between lanes stays out of the members)
+        if (B <= THREADS) {      // every thread has a window, and looks it up once
+            if (tid < B) {
+                my_L = cached_tokens(a.pages, tid);
+                my_R = live_rows(a.pages, tid);
+                mine = span_of<ST>(a, my_L, my_R).n * a.groups;
             }
-            if (threadIdx.x % 64 == 63) sums[threadIdx.x / 64] = incl;
-            if (threadIdx.x == 0) found[0] = -1;
-            __syncthreads();
-            int before = carry, all = 0;
-#pragma unroll
-            for (int v = 0; v < THREADS / 64; ++v) {
-                if (v < (int)threadIdx.x / 64) before += sums[v];
-                all += sums[v];
-            }
-            if (w >= before + incl - mine && w < before + incl) found[0] = b, found[1] = before + incl - mine;
-            __syncthreads();
-            b_out = found[0], start_out = found[1];
-            carry += all;
-            __syncthreads();
-            if (b_out >= 0) break;
+        } else {
+            for (int i = tid; i < B; i += THREADS) mine += span_of<ST>(a, i).n * a.groups;
         }
-        b_out = uniform(b_out);
-        start_out = uniform(start_out);
+        scan(mine, sums, before, all);
+        total = uniform(all);
+        const int most = uniform(total / a.least);
+        cuts = most < 1 ? 1 : most < clusters ? most : clusters;
+        if (cluster >= cuts) return false;
+        w = cut(cluster, total, cuts);
+        w_end = cut(cluster + 1, total, cuts);
+        if (w >= w_end) return false;
+        if (B <= THREADS) {
+            if (w >= before && w < before + mine) found[0] = tid, found[1] = before, found[2] = my_L, found[3] = my_R;
+            __syncthreads();
+        } else {
+            for (int base = 0, carry = 0;; base += THREADS, carry += all) {      // (w is somewhere)
+                const int i = base + tid;
+                my_L = i < B ? cached_tokens(a.pages, i) : 0;
+                my_R = i < B ? live_rows(a.pages, i) : 0;
+                mine = span_of<ST>(a, my_L, my_R).n * a.groups;
+                __syncthreads();
+                scan(mine, sums, before, all);
+                before += carry;
+                if (w >= before && w < before + mine) found[0] = i, found[1] = before, found[2] = my_L, found[3] = my_R;
+                if (w < carry + all) break;
+            }
+            __syncthreads();
+        }
+        b = uniform(found[0]);
+        start = uniform(found[1]);
+        L = uniform(found[2]);
+        R = uniform(found[3]);
+        return true;
     }
 };
 
@@ -275,10 +306,14 @@ __device__ __forceinline__ f32x4 four(const char *at)
     }
 }
 
-// The line's `total` places are cut into `cuts` pieces that differ by one place at most: the first place of a piece, and the piece of a place.
-// (Products are below 2^46 and quotients below 2^15: in fp64 no quotient is rounded to a whole number that it does not reach.)
-__device__ __forceinline__ int cut(int piece, int total, int cuts) { return uniform((int)((double)piece * total / cuts)); }
-__device__ __forceinline__ int piece_of(int place, int total, int cuts) { return uniform((int)((((double)place + 1.0) * cuts - 1.0) / total)); }
+// row of vector x: x / G.  (x < 2^20 and G <= 1024: x + 1/2 is further from the next multiple of G than the two roundings can carry it)
+__device__ __forceinline__ int row_of(const AttendArgs &a, int x) { return (int)(((float)x + 0.5f) * a.inv_G); }
+// ... and its number among all rows' query heads
+__device__ __forceinline__ int64_t vector_of(const AttendArgs &a, int b, int kvh, int x)
+{
+    const int r = row_of(a, x);
+    return ((int64_t)b * a.pages.rows + r) * a.n_q + kvh * a.G + x - r * a.G;
+}
 
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
@@ -359,28 +394,24 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
     constexpr bool F32 = F::TYPE == CACHE_F32;
     __shared__ __attribute__((aligned(1024))) char lds[F::LDS];
     __shared__ Segment<F> pages;
-    __shared__ int sums[F::WAVES + 3];
+    __shared__ int sums[F::WAVES], found[4];
     __shared__ int wflag[2][F::WAVES];
     __shared__ float mls[2][F::WK][QB];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
     const int wq = wave % F::WQ, wk = wave / F::WQ;
-    const int G = a.n_q / a.n_kv, words = (a.pages.rows + 31) / 32;
+    const int G = a.G, words = (a.pages.rows + 31) / 32;
     const int cap = a.pages.width << a.pages.log_page, page = 1 << a.pages.log_page;
 
     // this workgroup's piece of the line of tiles; its block of vectors
     const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, per_xcd = a.clusters / 8;
     const int members = a.heads * a.blocks, cluster = uniform(xcd * per_xcd + place / members), member = uniform(place % members);
     const int block = uniform(member % a.blocks), head_of_group = uniform(member / a.blocks);
-    const Line<ST, F::THREADS> line{sums};
-    const int total = uniform(line.total(a)), most = uniform(total / a.least), cuts = most < 1 ? 1 : most < a.clusters ? most : a.clusters;
-    if (cluster >= cuts) return;
-    int w = cut(cluster, total, cuts);
-    const int w_end = cut(cluster + 1, total, cuts);
-    if (w >= w_end) return;
-    int b, start;
-    line.find(a, w, b, start);
-    Span sp = span_of<ST>(a, b);
+    Line<ST, F::THREADS> line;
+    if (!line.begin(a, cluster, a.clusters, sums, found)) return;
+    const int total = line.total, cuts = line.cuts, w_end = line.w_end;
+    int w = line.w, b = line.b, start = line.start;
+    Span sp = span_of<ST>(a, line.L, line.R);
 
     const uint32_t lds0 = lds_offset_of(lds);
     const float c = a.score_scale, threshold = 8.f / c;
@@ -413,7 +444,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
         const int nvec = sp.R * G;
         if (block * QB >= nvec) continue;
         const int x_last = (block + 1) * QB < nvec ? (block + 1) * QB - 1 : nvec - 1;
-        const int r_first = block * QB / G, r_last = x_last / G;
+        const int r_first = uniform(row_of(a, block * QB)), r_last = uniform(row_of(a, x_last));
 
         // the visits that this block needs: not those behind its last row, nor those before its first row's window; among them, from i_full to i_part, the
         // tiles of which every row of the block sees everything
@@ -437,7 +468,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
         }
 
         // queries as the B operand: column = vector
-        const int x = block * QB + wq * 32 + col, xc = x < nvec ? x : nvec - 1, r = xc / G, head = kvh * G + xc % G;
+        const int x = block * QB + wq * 32 + col, xc = x < nvec ? x : nvec - 1, r = row_of(a, xc), head = kvh * G + xc - r * G;
         const bool active = block * QB + wq * 32 < nvec;
         const int64_t vec = ((int64_t)b * a.pages.rows + r) * a.n_q + head;
         u32x4 q[F::QREGS];
@@ -601,22 +632,26 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                             for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[db], s[kb][e], acc[db], 0, 0, 0);
                         }
                 } else {
-                    constexpr int KS = KT / 16;
+                    // DG blocks of 32 elements at a time: their fragments are asked for while the products before them run
+                    constexpr int KS = KT / 16, DG = DB < 4 ? DB : 4, STEPS = KS * DB / DG;
                     const uint32_t base = vt + values_base<F>(here(lane));
-                    bf16x8 y[2][DB];
+                    bf16x8 y[2][DG], p;
+                    const auto ask = [&](int n) ALWAYS_INLINE {
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) y[0][db] = values<F>(base, 0, db);
+                        for (int j = 0; j < DG; ++j) y[n & 1][j] = values<F>(base, n / (DB / DG), n % (DB / DG) * DG + j);
+                    };
+                    ask(0);
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        bf16x8 p;      // weights lose at most half a step of bf16, 2^-8 of each: as the products' operand they have to
+                    for (int n = 0; n < STEPS; ++n) {
+                        const int ks = n / (DB / DG), d0 = n % (DB / DG) * DG;
+                        if (d0 == 0) {
+                            // weights lose at most half a step of bf16, 2^-8 of each: as the products' operand they have to
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[ks / 2][8 * (ks & 1) + e];
-                        if (ks + 1 < KS) {
-#pragma unroll
-                            for (int db = 0; db < DB; ++db) y[(ks + 1) & 1][db] = values<F>(base, ks + 1, db);
+                            for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[ks / 2][8 * (ks & 1) + e];
                         }
+                        if (n + 1 < STEPS) ask(n + 1);
 #pragma unroll
-                        for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[ks & 1][db], p, acc[db], 0, 0, 0);
+                        for (int j = 0; j < DG; ++j) acc[d0 + j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[n & 1][j], p, acc[d0 + j], 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
@@ -683,7 +718,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                 const char *vt = tile + F::TILE + wk * KT * RB;
                 score(lds_offset_of(tile) + wk * KT * RB);
                 uint32_t vis[NKB];      // bit e: the lane's row sees token e of the 32
-                const int r = (block * QB + wq * 32 + (here(lane) & 31) < nvec ? block * QB + wq * 32 + (here(lane) & 31) : nvec - 1) / G;
+                const int xm = block * QB + wq * 32 + (here(lane) & 31), r = row_of(a, xm < nvec ? xm : nvec - 1);
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb) {
                     const int t = t_tile + wk * KT + 32 * kb;
@@ -788,9 +823,11 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     *(f32x4 *)(merge + (8 * db + 2 * e) * QB * 4) =
                         f32x4{acc[db][4 * e] * mine, acc[db][4 * e + 1] * mine, acc[db][4 * e + 2] * mine, acc[db][4 * e + 3] * mine};
             __syncthreads();
-            for (int e = here(tid); e < F::DP / 4 * QB; e += F::THREADS) {
-                const int d4 = e / QB, xl = e % QB, xx = block * QB + xl;
-                if (xx >= nvec) continue;
+            // (as many vectors as there are, rounded up to a power of two)
+            const int nv = x_last + 1 - block * QB, log_nv = nv > 1 ? 32 - __builtin_clz(nv - 1) : 0;
+            for (int e = here(tid); e < (a.D / 4) << log_nv; e += F::THREADS) {
+                const int d4 = e >> log_nv, xl = e & ((1 << log_nv) - 1), xx = block * QB + xl;
+                if (xl >= nv) continue;
                 float tm = -INFINITY, tl = 0.f;
 #pragma unroll
                 for (int v = 0; v < F::WK; ++v) tm = fmaxf(tm, mls[0][v][xl]);
@@ -801,9 +838,9 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     tl += mls[1][v][xl] * (mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mv - tm) * c));
                     o += *(const f32x4 *)((float *)lds + ((v * (F::DP / 4) + d4) * QB + xl) * 4);
                 }
-                const int64_t vx = ((int64_t)b * a.pages.rows + xx / G) * a.n_q + kvh * G + xx % G;
+                const int64_t vx = vector_of(a, b, kvh, xx);
                 if (whole) finish<F::TYPE>(a, vx, d4, o, tl);
-                else mine_part.store(e, o);
+                else mine_part.store(d4 * QB + xl, o);
                 if (d4 == 0) {
                     if (whole) finish_lse(a, vx, tm * c, tl);
                     else mine_part.store(xl, tm * c, tl);
@@ -827,10 +864,10 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
         const int xl = here(tid) & ((1 << log_nv) - 1), first = here(tid) >> log_nv, step = F::THREADS >> log_nv;
         if (xl >= nv) continue;
         const int xx = block * QB + xl;
-        const int64_t vx = ((int64_t)b * a.pages.rows + xx / G) * a.n_q + kvh * G + xx % G;
+        const int64_t vx = vector_of(a, b, kvh, xx);
         const auto part = [&](int cl) ALWAYS_INLINE { return Part(a, unit(cl), QB, F::DP); };
         if (step >= a.D / 4) {
-            if (first < a.D / 4) join<F, 16, 1>(a, part, c0, c1, xl, vx, first, step);
+            if (first < a.D / 4) join<F, (F::WK > 1 ? 32 : 16), 1>(a, part, c0, c1, xl, vx, first, step);
         } else {
             for (int d0 = first; d0 < a.D / 4; d0 += 4 * step) join<F, 8, 4>(a, part, c0, c1, xl, vx, d0, step);
         }

@@ -302,3 +302,25 @@ def test_refusals():
     assert lib.aj_cache_append(empty, None, None, None, None, None, 0.0, None, None, None, None, None, 1.0, 1.0, None, None, None, None) == 0
     assert lib.aj_cache_commit(empty, None, None, None, None, 1, 0, None, None, None, None) == 0
     aj.aj_cache_destroy(empty)
+
+
+@pytest.mark.parametrize("B", [128, 129, 256, 257, 600])
+def test_many_windows(B):
+    """More windows than a workgroup has threads; some without rows."""
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 90, (B,), generator=g).tolist()
+    rows = torch.randint(0, 3, (B,), generator=g).tolist()
+    c = ref.Cache(B, K=1, B=B, page=8, lens=lens, rows=rows, n_q=2, n_kv=1, D=64)
+    poison(c)
+    q = queries(c)
+    kw = dict(scale=0.2)
+    check(c, q, *run(c, q, **kw), **kw)
+    c = ref.Cache(B, type="f32", K=20, B=B, page=8, lens=[n % 7 for n in lens], rows=[20 * n for n in rows], n_q=2, n_kv=1, D=16)
+    q = queries(c)
+    check(c, q, *run(c, q, **kw), **kw)
+
+
+def test_no_rows_at_all():
+    c = ref.Cache(1, K=2, B=3, lens=(4, 0, 9), rows=(0, 0, -2), n_q=2, n_kv=1, D=64)
+    q = queries(c)
+    check(c, q, *run(c, q, scale=0.2), scale=0.2)
