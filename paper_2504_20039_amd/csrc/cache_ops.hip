@@ -159,16 +159,13 @@ hipError_t cache_append(CacheType type, const AppendArgs &a, hipStream_t s)
 __device__ __forceinline__ int tree_word(int r, int w) { return (16 * (r / 32) + r % 32) * (r / 32 + 1) + w; }
 
 template <int ROWS, int THREADS>
-__global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, const int32_t *parent, int32_t *depth, uint32_t *mask)
+__global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, int log_words, const int32_t *parent, int32_t *depth, uint32_t *mask)
 {
     __shared__ uint32_t bits[16 * (ROWS / 32) * (ROWS / 32 + 1)];
     __shared__ int16_t up[2][ROWS];
-    const int words = (rows + 31) / 32, n = rows * words, tid = threadIdx.x;
+    // a thread has one word of every `step`-th row (words rounded up to a power of two)
+    const int words = (rows + 31) / 32, tid = threadIdx.x, w = tid & ((1 << log_words) - 1), first = tid >> log_words, step = THREADS >> log_words;
     const int32_t *mine = parent + (int64_t)blockIdx.x * (rows - 1);
-    for (int i = tid; i < n; i += THREADS) {
-        const int r = i / words, w = i % words;
-        if (w <= r / 32) bits[tree_word(r, w)] = w == r / 32 ? 1u << (r & 31) : 0u;
-    }
     for (int r = tid; r < rows; r += THREADS) {
         int p = -1;
         if (r) {
@@ -177,11 +174,14 @@ __global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, const int3
         }
         up[0][r] = (int16_t)p;
     }
+    for (int r = first; r < rows; r += step)
+        if (w <= r / 32) bits[tree_word(r, w)] = w == r / 32 ? 1u << (r & 31) : 0u;
     __syncthreads();
     int from = 0;
     for (int reach = 1; reach < rows; reach *= 2, from ^= 1) {
-        for (int i = tid; i < n; i += THREADS) {
-            const int r = i / words, w = i % words, p = up[from][r];
+#pragma unroll 4
+        for (int r = first; r < rows; r += step) {
+            const int p = up[from][r];
             if (p >= 0 && w <= p / 32) bits[tree_word(r, w)] |= bits[tree_word(p, w)];
         }
         for (int r = tid; r < rows; r += THREADS) {
@@ -190,23 +190,23 @@ __global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, const int3
         }
         __syncthreads();
     }
-    for (int i = tid; i < n; i += THREADS) {
-        const int r = i / words, w = i % words;
-        mask[(int64_t)blockIdx.x * n + i] = w <= r / 32 ? bits[tree_word(r, w)] : 0u;
-    }
+    for (int r = first; r < rows; r += step)
+        if (w < words) mask[((int64_t)blockIdx.x * rows + r) * words + w] = w <= r / 32 ? bits[tree_word(r, w)] : 0u;
     for (int r = tid; r < rows; r += THREADS) {
         int count = -1;
-        for (int w = 0; w <= r / 32; ++w) count += __popc(bits[tree_word(r, w)]);
+        for (int v = 0; v <= r / 32; ++v) count += __popc(bits[tree_word(r, v)]);
         depth[(int64_t)blockIdx.x * rows + r] = count;
     }
 }
 
 hipError_t tree_mask(int B, int K, const int32_t *parent, int32_t *depth, uint32_t *mask, hipStream_t s)
 {
-    const int rows = K + 1;
-    if (rows <= 64) tree_mask_kernel<64, 64><<<B, 64, 0, s>>>(rows, parent, depth, mask);
-    else if (rows <= 256) tree_mask_kernel<256, 256><<<B, 256, 0, s>>>(rows, parent, depth, mask);
-    else tree_mask_kernel<1024, 1024><<<B, 1024, 0, s>>>(rows, parent, depth, mask);
+    const int rows = K + 1, words = (rows + 31) / 32;
+    int log_words = 0;
+    while ((1 << log_words) < words) ++log_words;
+    if (rows <= 64) tree_mask_kernel<64, 64><<<B, 64, 0, s>>>(rows, log_words, parent, depth, mask);
+    else if (rows <= 256) tree_mask_kernel<256, 512><<<B, 512, 0, s>>>(rows, log_words, parent, depth, mask);
+    else tree_mask_kernel<1024, 1024><<<B, 1024, 0, s>>>(rows, log_words, parent, depth, mask);
     return hipGetLastError();
 }
 
