@@ -159,12 +159,13 @@ hipError_t cache_append(CacheType type, const AppendArgs &a, hipStream_t s)
 __device__ __forceinline__ int tree_word(int r, int w) { return (16 * (r / 32) + r % 32) * (r / 32 + 1) + w; }
 
 template <int ROWS, int THREADS>
-__global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, int log_words, const int32_t *parent, int32_t *depth, uint32_t *mask)
+__global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, const int32_t *parent, int32_t *depth, uint32_t *mask)
 {
     __shared__ uint32_t bits[16 * (ROWS / 32) * (ROWS / 32 + 1)];
     __shared__ int16_t up[2][ROWS];
-    // a thread has one word of every `step`-th row (words rounded up to a power of two)
-    const int words = (rows + 31) / 32, tid = threadIdx.x, w = tid & ((1 << log_words) - 1), first = tid >> log_words, step = THREADS >> log_words;
+    // a thread has one word of every STEP-th row
+    constexpr int WORDS = ROWS / 32, STEP = THREADS / WORDS, MINE = ROWS / STEP;
+    const int words = (rows + 31) / 32, tid = threadIdx.x, w = tid % WORDS, first = tid / WORDS;
     const int32_t *mine = parent + (int64_t)blockIdx.x * (rows - 1);
     for (int r = tid; r < rows; r += THREADS) {
         int p = -1;
@@ -174,15 +175,27 @@ __global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, int log_wo
         }
         up[0][r] = (int16_t)p;
     }
-    for (int r = first; r < rows; r += step)
-        if (w <= r / 32) bits[tree_word(r, w)] = w == r / 32 ? 1u << (r & 31) : 0u;
+    // it keeps its words in registers, so that a round's reads do not wait for its writes
+    uint32_t own[MINE];
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+        const int r = first + k * STEP;
+        own[k] = w == r / 32 ? 1u << (r & 31) : 0u;
+        if (r < rows && w <= r / 32) bits[tree_word(r, w)] = own[k];
+    }
     __syncthreads();
     int from = 0;
     for (int reach = 1; reach < rows; reach *= 2, from ^= 1) {
-#pragma unroll 4
-        for (int r = first; r < rows; r += step) {
-            const int p = up[from][r];
-            if (p >= 0 && w <= p / 32) bits[tree_word(r, w)] |= bits[tree_word(p, w)];
+        int p[MINE];
+        uint32_t y[MINE];
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) p[k] = first + k * STEP < rows ? up[from][first + k * STEP] : -1;
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) y[k] = p[k] >= 0 && w <= p[k] / 32 ? bits[tree_word(p[k], w)] : 0u;
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            own[k] |= y[k];
+            if (p[k] >= 0 && w <= p[k] / 32) bits[tree_word(first + k * STEP, w)] = own[k];
         }
         for (int r = tid; r < rows; r += THREADS) {
             const int p = up[from][r];
@@ -190,8 +203,9 @@ __global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, int log_wo
         }
         __syncthreads();
     }
-    for (int r = first; r < rows; r += step)
-        if (w < words) mask[((int64_t)blockIdx.x * rows + r) * words + w] = w <= r / 32 ? bits[tree_word(r, w)] : 0u;
+#pragma unroll
+    for (int k = 0; k < MINE; ++k)
+        if (first + k * STEP < rows && w < words) mask[((int64_t)blockIdx.x * rows + first + k * STEP) * words + w] = own[k];
     for (int r = tid; r < rows; r += THREADS) {
         int count = -1;
         for (int v = 0; v <= r / 32; ++v) count += __popc(bits[tree_word(r, v)]);
@@ -201,12 +215,12 @@ __global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, int log_wo
 
 hipError_t tree_mask(int B, int K, const int32_t *parent, int32_t *depth, uint32_t *mask, hipStream_t s)
 {
-    const int rows = K + 1, words = (rows + 31) / 32;
-    int log_words = 0;
-    while ((1 << log_words) < words) ++log_words;
-    if (rows <= 64) tree_mask_kernel<64, 64><<<B, 64, 0, s>>>(rows, log_words, parent, depth, mask);
-    else if (rows <= 256) tree_mask_kernel<256, 512><<<B, 512, 0, s>>>(rows, log_words, parent, depth, mask);
-    else tree_mask_kernel<1024, 1024><<<B, 1024, 0, s>>>(rows, log_words, parent, depth, mask);
+    const int rows = K + 1;
+    if (rows <= 64) tree_mask_kernel<64, 64><<<B, 64, 0, s>>>(rows, parent, depth, mask);
+    else if (rows <= 128) tree_mask_kernel<128, 256><<<B, 256, 0, s>>>(rows, parent, depth, mask);
+    else if (rows <= 256) tree_mask_kernel<256, 512><<<B, 512, 0, s>>>(rows, parent, depth, mask);
+    else if (rows <= 512) tree_mask_kernel<512, 1024><<<B, 1024, 0, s>>>(rows, parent, depth, mask);
+    else tree_mask_kernel<1024, 1024><<<B, 1024, 0, s>>>(rows, parent, depth, mask);
     return hipGetLastError();
 }
 

@@ -132,7 +132,7 @@ def test_append_in_place_and_nowhere():
         assert torch.equal(after.view(torch.uint8)[left], before[i][left])
 
 
-@pytest.mark.parametrize("K", [1, 2, 31, 32, 63, 64, 200, 255, 256, 511, 1023])
+@pytest.mark.parametrize("K", [1, 2, 31, 32, 63, 64, 127, 128, 200, 255, 256, 500, 511, 512, 1023])
 @pytest.mark.parametrize("shape", ["near", "any", "chain", "star", "bad"])
 def test_tree_mask(K, shape):
     import paper_2504_20039_amd as aj
