@@ -70,7 +70,7 @@ struct AttendArgs {
     // the line of tiles is cut into `clusters` pieces; a cluster has a workgroup for each of `heads` heads of keys and values and `blocks` blocks of
     // vectors; groups = n_kv / heads.  Partial results of two items per piece
     int clusters, heads, groups, blocks;
-    int least;             // tiles of a piece at least
+    float part_cost;       // what adding a part of an item takes, in tiles
     float *part_o;         // [clusters][2][heads][blocks][head size / 4][vectors of a block][4]
     float2 *part_ml;       // [clusters][2][heads][blocks][vectors of a block]
     int *arrived;          // [clusters][heads][blocks], zero between calls

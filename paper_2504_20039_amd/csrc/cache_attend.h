@@ -261,7 +261,9 @@ struct Line {
         }
         scan(mine, sums, before, all);
         total = uniform(all);
-        const int most = uniform(total / a.least);
+        // A piece of an item of n tiles that is cut into pieces of x tiles takes x tiles' time, and its join n / x parts' time: together least at
+        // x = sqrt(n * a part's time / a tile's)
+        const int least = uniform((int)sqrtf((float)total / (B * a.groups) * a.part_cost)), most = uniform(total / (least < 1 ? 1 : least));
         cuts = most < 1 ? 1 : most < clusters ? most : clusters;
         if (cluster >= cuts) return false;
         w = cut(cluster, total, cuts);
@@ -352,7 +354,7 @@ __device__ __forceinline__ void join(const AttendArgs &a, const P &part, int c0,
         f32x4 y[PARTS][PIECES];
 #pragma unroll
         for (int j = 0; j < PARTS; ++j) {
-            const Part one = part(cl + j < c1 ? cl + j : c1);      // (the last part once more counts for nothing)
+            const Part one = part(cl + j < c1 ? cl + j : c1);      // (the last part once more, which is then left out)
             ml[j] = one.load_ml(xl);
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) y[j][p] = one.load((d0 + p * step < F::DP / 4 ? d0 + p * step : 0) * F::QB + xl);
@@ -368,10 +370,12 @@ __device__ __forceinline__ void join(const AttendArgs &a, const P &part, int c0,
         for (int p = 0; p < PIECES; ++p) o[p] *= keep;
 #pragma unroll
         for (int j = 0; j < PARTS; ++j) {
-            const float f = ml[j].x == -INFINITY || cl + j > c1 ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - m);
-            l += ml[j].y * f;
+            const float f = ml[j].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - m);
+            if (cl + j <= c1) {      // (no product with zero: the part may be infinite)
+                l += ml[j].y * f;
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) o[p] += y[j][p] * f;
+                for (int p = 0; p < PIECES; ++p) o[p] += y[j][p] * f;
+            }
         }
     }
 #pragma unroll
