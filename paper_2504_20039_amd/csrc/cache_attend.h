@@ -37,19 +37,21 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(4))) short i16x4;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 
-// DP: head size, padded; WQ x WK waves: WQ blocks of 32 vectors, WK parts of KT tokens of a tile
-template <CacheType TYPE_, int DP_, int WQ_, int WK_, int KT_, int NST_, int PER_CU_>
+// DP: head size, padded; WQ x WK x WD waves: WQ blocks of 32 vectors, WK parts of KT tokens of a tile, WD parts of the head size: those waves make the same
+// scores, each for its own part of O.  At DP = 256 all of O for 32 vectors leaves a wave too few registers for its loads' addresses, which then come back
+// from memory between the loads: with WD = 2, 21 windows x 1 row x 8 heads over 5000 tokens of 4 heads take 86 us (5.0 TB/s) instead of 215
+template <CacheType TYPE_, int DP_, int WQ_, int WK_, int KT_, int NST_, int PER_CU_, int WD_ = 1>
 struct Form {
     static constexpr CacheType TYPE = TYPE_;
-    static constexpr int DP = DP_, WQ = WQ_, WK = WK_, KT = KT_, NST = NST_, PER_CU = PER_CU_;
+    static constexpr int DP = DP_, WQ = WQ_, WK = WK_, WD = WD_, KT = KT_, NST = NST_, PER_CU = PER_CU_;
     static constexpr int KES = TYPE == CACHE_FP8 ? 1 : TYPE == CACHE_F32 ? 4 : 2;
-    static constexpr int WAVES = WQ * WK, THREADS = 64 * WAVES, QB = 32 * WQ, ST = WK * KT;
+    static constexpr int WAVES = WQ * WK * WD, THREADS = 64 * WAVES, QB = 32 * WQ, ST = WK * KT;
     static constexpr int RB = DP * KES, CPR = RB / 16, RPI = 64 / CPR;        // bytes and chunks of a row, rows of a load instruction
     static constexpr int TILE = ST * RB, STAGE = 2 * TILE;                    // keys, then values
     static constexpr int NI = TILE / 1024 / WAVES;                            // load instructions of a wave for the keys of a tile (values: the same)
-    static constexpr int NKB = KT / 32, DB = DP / 32, QREGS = TYPE == CACHE_F32 ? DP / 8 : DP / 16;
+    static constexpr int NKB = KT / 32, DB = DP / 32 / WD, QREGS = TYPE == CACHE_F32 ? DP / 8 : DP / 16;
     static constexpr int SEG = 1024;                                          // pages in LDS
-    static constexpr int MERGE = WK > 1 ? WAVES * DP * 32 * 4 : 0;            // bytes to add up the waves' parts
+    static constexpr int MERGE = WK > 1 ? WQ * WK * DP * 32 * 4 : 0;            // bytes to add up the waves' parts
     static constexpr int LDS = NST * STAGE > MERGE ? NST * STAGE : MERGE;
     static_assert(TILE % (1024 * WAVES) == 0 && CPR <= 64 && 2 * NI * (NST - 1) < 64, "whole load instructions, vmcnt");
 };
@@ -71,6 +73,11 @@ __device__ __forceinline__ int f_v(int row)
 __device__ __forceinline__ void load_to_lds_16_at(const char *at, uint32_t lds_dst)
 {
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds_dst) : "memory");
+}
+
+__device__ __forceinline__ void load_to_lds_16_at_nt(const char *at, uint32_t lds_dst)
+{
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(at), "s"(lds_dst) : "memory");
 }
 
 // maximum and sum of the lane's value and that of the lane 32 away (swapping the halves of two copies leaves each half's values in both)
@@ -403,7 +410,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
     __shared__ float mls[2][F::WK][QB];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
-    const int wq = wave % F::WQ, wk = wave / F::WQ;
+    const int wq = wave % F::WQ, wk = wave / F::WQ % F::WK, wd = wave / (F::WQ * F::WK), db0 = wd * DB;      // db0: the wave's first 32 elements of O
     const int G = a.G, words = (a.pages.rows + 31) / 32;
     const int cap = a.pages.width << a.pages.log_page, page = 1 << a.pages.log_page;
 
@@ -545,13 +552,23 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     }
                 } else {
                     const int row0 = wave * NI * F::RPI + here(lane) / F::CPR;
-                    int64_t at[NI];
+                    constexpr int BATCH = NI < 4 ? NI : 4;
 #pragma unroll
-                    for (int n = 0; n < NI; ++n) at[n] = pages.at[page_of(i, row0 + n * F::RPI)];
+                    for (int n0 = 0; n0 < NI; n0 += BATCH) {
+                        int64_t at[BATCH];
 #pragma unroll
-                    for (int n = 0; n < NI; ++n) {
-                        load_to_lds_16_at(k_head + (at[n] + (uint32_t)here(k_off[n])), dst + n * 1024);
-                        load_to_lds_16_at(v_head + (at[n] + (uint32_t)here(v_off[n])), dst + n * 1024 + F::TILE);
+                        for (int n = 0; n < BATCH; ++n) at[n] = pages.at[page_of(i, row0 + (n0 + n) * F::RPI)];
+#pragma unroll
+                        for (int n = 0; n < BATCH; ++n) {
+                            const char *k = k_head + (at[n] + (uint32_t)here(k_off[n0 + n])), *v = v_head + (at[n] + (uint32_t)here(v_off[n0 + n]));
+                            if (once) {
+                                load_to_lds_16_at_nt(k, dst + (n0 + n) * 1024);
+                                load_to_lds_16_at_nt(v, dst + (n0 + n) * 1024 + F::TILE);
+                            } else {
+                                load_to_lds_16_at(k, dst + (n0 + n) * 1024);
+                                load_to_lds_16_at(v, dst + (n0 + n) * 1024 + F::TILE);
+                            }
+                        }
                     }
                 }
             };
@@ -623,7 +640,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
             // O^T += V^T P^T
             const auto add = [&](uint32_t vt) ALWAYS_INLINE {
                 if constexpr (F32) {
-                    const uint32_t base = vt + here(4 * h * RB + ((col >> 2) ^ (h << 3)) * 16 + (col & 3) * 4);
+                    const uint32_t base = (vt + here(4 * h * RB + ((col >> 2) ^ (h << 3)) * 16 + (col & 3) * 4)) ^ (128 * db0);
 #pragma unroll
                     for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
@@ -638,7 +655,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                 } else {
                     // DG blocks of 32 elements at a time: their fragments are asked for while the products before them run
                     constexpr int KS = KT / 16, DG = DB < 4 ? DB : 4, STEPS = KS * DB / DG;
-                    const uint32_t base = vt + values_base<F>(here(lane));
+                    const uint32_t base = (vt + values_base<F>(here(lane))) ^ (32 * db0 * F::KES);
                     bf16x8 y[2][DG], p;
                     const auto ask = [&](int n) ALWAYS_INLINE {
 #pragma unroll
@@ -785,7 +802,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     for (int db = 0; db < DB; ++db)
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
-                            const int at = (32 * db + 8 * g + 4 * h) * F::KES;
+                            const int at = (32 * (db0 + db) + 8 * g + 4 * h) * F::KES;
                             const f32x4 y = four<F>(row + ((at / 16) ^ f) * 16 + at % 16);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) acc[db][4 * g + j] = seen ? fmaf(p, y[j], acc[db][4 * g + j]) : acc[db][4 * g + j];
@@ -808,24 +825,24 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const f32x4 o = {acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]};
-                        const int d4 = 8 * db + 2 * e + h;
+                        const int d4 = 8 * (db0 + db) + 2 * e + h;
                         if (whole) finish<F::TYPE>(a, vec, d4, o, l);
                         else mine_part.store(d4 * QB + wq * 32 + col, o);
                     }
-                if (h == 0) {
+                if (h == 0 && wd == 0) {
                     if (whole) finish_lse(a, vec, m * c, l);
                     else mine_part.store(wq * 32 + col, m * c, l);
                 }
             }
         } else {
             __syncthreads();      // the stages are free
-            if (h == 0) mls[0][wk][wq * 32 + col] = m, mls[1][wk][wq * 32 + col] = l;
+            if (h == 0 && wd == 0) mls[0][wk][wq * 32 + col] = m, mls[1][wk][wq * 32 + col] = l;
             __syncthreads();
             float top = -INFINITY;
 #pragma unroll
             for (int v = 0; v < F::WK; ++v) top = fmaxf(top, mls[0][v][wq * 32 + col]);
             const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
-            float *merge = (float *)lds + ((wk * (F::DP / 4) + (here(lane) >> 5)) * QB + wq * 32 + (here(lane) & 31)) * 4;      // [WK][DP/4][QB][4]
+            float *merge = (float *)lds + ((wk * (F::DP / 4) + 8 * db0 + (here(lane) >> 5)) * QB + wq * 32 + (here(lane) & 31)) * 4;      // [WK][DP/4][QB][4]
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll

@@ -6,7 +6,7 @@ namespace aj {
 template <int DP, bool FEW> struct Choice;
 template <> struct Choice<64, true> { typedef Form<CACHE_F32, 64, 1, 2, 32, 2, 2> F; };
 template <> struct Choice<128, true> { typedef Form<CACHE_F32, 128, 1, 2, 32, 2, 1> F; };
-template <> struct Choice<256, true> { typedef Form<CACHE_F32, 256, 4, 1, 32, 2, 1> F; };
+template <> struct Choice<256, true> { typedef Form<CACHE_F32, 256, 1, 1, 32, 2, 1, 4> F; };
 template <> struct Choice<64, false> { typedef Form<CACHE_F32, 64, 4, 1, 64, 2, 2> F; };
 template <> struct Choice<128, false> { typedef Form<CACHE_F32, 128, 4, 1, 64, 2, 1> F; };
 template <> struct Choice<256, false> { typedef Form<CACHE_F32, 256, 4, 1, 32, 2, 1> F; };

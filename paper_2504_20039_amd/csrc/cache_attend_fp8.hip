@@ -6,7 +6,7 @@ namespace aj {
 template <int DP, bool FEW> struct Choice;
 template <> struct Choice<64, true> { typedef Form<CACHE_FP8, 64, 1, 4, 32, 2, 2> F; };
 template <> struct Choice<128, true> { typedef Form<CACHE_FP8, 128, 1, 4, 32, 2, 2> F; };
-template <> struct Choice<256, true> { typedef Form<CACHE_FP8, 256, 1, 2, 32, 2, 2> F; };
+template <> struct Choice<256, true> { typedef Form<CACHE_FP8, 256, 1, 2, 32, 2, 2, 2> F; };
 template <> struct Choice<64, false> { typedef Form<CACHE_FP8, 64, 4, 1, 64, 2, 2> F; };
 template <> struct Choice<128, false> { typedef Form<CACHE_FP8, 128, 4, 1, 64, 2, 2> F; };
 template <> struct Choice<256, false> { typedef Form<CACHE_FP8, 256, 4, 1, 32, 4, 1> F; };

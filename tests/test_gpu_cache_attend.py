@@ -193,9 +193,10 @@ def test_pages_outside_the_window_may_be_gone():
 
 @pytest.mark.parametrize("type", ["bf16", "f32", "fp8"])
 @pytest.mark.parametrize("K", [5, 40])
-def test_nan_and_infinity_in_tokens_that_a_row_does_not_see(type, K):
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_nan_and_infinity_in_tokens_that_a_row_does_not_see(type, K, D):
     """A draft row whose state overflowed: rows that do not see it are as if it were not there, rows that do are NaN or infinite."""
-    c = ref.Cache(17, type=type, K=K, B=2, lens=(60, 100), n_q=8, n_kv=2, D=128)
+    c = ref.Cache(17, type=type, K=K, B=2, lens=(60, 100), n_q=8, n_kv=2, D=D)
     q = queries(c)
     kw = dict(scale=0.1)
     want, want_lse, tol, lse_tol = ref.attend(c, q, **kw)      # without them
