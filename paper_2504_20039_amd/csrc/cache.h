@@ -71,6 +71,7 @@ struct AttendArgs {
     // vectors; groups = n_kv / heads.  Partial results of two items per piece
     int clusters, heads, groups, blocks;
     float part_cost;       // what adding a part of an item takes, in tiles
+    float whole;           // items of as many tiles or fewer are not cut
     float *part_o;         // [clusters][2][heads][blocks][head size / 4][vectors of a block][4]
     float2 *part_ml;       // [clusters][2][heads][blocks][vectors of a block]
     int *arrived;          // [clusters][heads][blocks], zero between calls

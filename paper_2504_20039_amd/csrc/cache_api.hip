@@ -240,6 +240,9 @@ extern "C" int aj_cache_attend(aj_cache *h, const void *q, const void *k_pool, c
     // Measured over one to four windows of 500 .. 30000 tokens (heads of 128 elements): few vectors 0.1 .. 0.2 (2 x 8 rows over 2500 tokens 30 us without, 26;
     // 0.4: 27), many in bf16 0.8 (32 rows over 2500 tokens 60, 35), in FP8 up to 0.4 (65 rows over 4000 tokens 40.6, 40.4; 0.8: 44), fp32, whose tiles take long, none
     a.part_cost = few ? 0.15f : h->type == CACHE_BF16 ? 0.8f : h->type == CACHE_FP8 ? 0.3f : 0.05f;
+    // Many vectors in 16 or 8 bits: an item of one or two tiles takes 17 us whole, 26 in two pieces, of four 23 and 28 (44 windows x 38 rows x 4 heads), of nine
+    // 35 and 28.  Few vectors take 13 in eight pieces and 19 whole (one row over 500 tokens)
+    a.whole = few || h->type == CACHE_F32 ? 1.f : 4.f;
     a.part_o = h->part_o;
     a.part_ml = h->part_ml;
     a.arrived = h->arrived;
