@@ -93,6 +93,18 @@ CASES = [
     dict(type="f32", K=40, B=2, lens=(100, 0), n_q=8, n_kv=2, D=64),
     dict(type="f32", K=70, B=1, lens=(77,), n_q=2, n_kv=1, D=128, order="hpsd"),
     dict(type="f32", K=34, B=2, lens=(5, 40), n_q=2, n_kv=2, D=256),
+    # items in two, a few and many pieces, equal ones and ragged ones
+    dict(type="bf16", K=37, B=5, lens=(1000, 600, 129, 0, 2100), n_q=4, n_kv=1, D=128),
+    dict(type="bf16", K=37, B=6, lens=(520,) * 6, n_q=8, n_kv=2, D=128, page=64),
+    dict(type="bf16", K=31, B=1, lens=(2500,), n_q=8, n_kv=2, D=64),
+    dict(type="bf16", K=40, B=2, lens=(900, 2000), n_q=4, n_kv=1, D=256),
+    dict(type="bf16", K=7, B=3, lens=(2500, 40, 700), n_q=4, n_kv=1, D=256, page=1),
+    dict(type="fp8", K=33, B=3, lens=(1500, 256, 700), n_q=16, n_kv=2, D=128),
+    dict(type="fp8", K=0, B=3, lens=(900, 20, 1700), n_q=16, n_kv=2, D=256, page=2),
+    dict(type="f32", K=33, B=2, lens=(600, 1200), n_q=2, n_kv=1, D=64),
+    dict(type="f32", K=33, B=1, lens=(700,), n_q=2, n_kv=1, D=256),
+    dict(type="f32", K=0, B=2, lens=(1500, 33), n_q=8, n_kv=1, D=256, page=4),
+    dict(type="f32", K=2, B=2, lens=(1500, 333), n_q=8, n_kv=1, D=128, rows=(3, 0)),
     # odd head sizes
     dict(type="bf16", K=5, B=2, lens=(64, 300), n_q=6, n_kv=2, D=80),
     dict(type="bf16", K=0, B=2, lens=(64, 300), n_q=5, n_kv=1, D=16),
