@@ -28,7 +28,6 @@ static bool plan_cache(const aj_cache_config &cfg, aj_cache *h)
     aj_cache_config &c = h->cfg;
     if (c.B < 0 || c.K < 0 || c.K > 1023 || (int64_t)c.B * (c.K + 1) >= (1 << 24)) return false;
     if (c.n_kv < 1 || c.n_q < 1 || c.n_q > 1024 || c.n_q % c.n_kv) return false;
-    if ((int64_t)(c.K + 1) * (c.n_q / c.n_kv) > (1 << 20)) return false;
     if (c.head_dim < 16 || c.head_dim > 256 || c.head_dim % 16) return false;
     if (c.dtype != AJ_F32 && c.dtype != AJ_BF16) return false;
     if (c.kv_dtype != AJ_KV_SAME && !(c.kv_dtype == AJ_KV_FP8_E4M3 && c.dtype == AJ_BF16)) return false;
@@ -227,7 +226,7 @@ extern "C" int aj_cache_attend(aj_cache *h, const void *q, const void *k_pool, c
     a.G = c.n_q / c.n_kv;
     a.inv_G = 1.f / (float)a.G;
     a.D = c.head_dim;
-    a.window = c.window;
+    a.window = c.window < 0x7fff0400 ? c.window : 0x7fff0400;      // beyond every position, and differences stay within 32 bits
     a.sinks = c.sinks;
     a.q_stride = c.q_stride;
     a.score_scale = score_scale;

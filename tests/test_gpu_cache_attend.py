@@ -120,6 +120,8 @@ CASES = [
     dict(type="bf16", K=70, B=2, lens=(300, 20), n_q=4, n_kv=1, D=64, window=50, sinks=130, rows=(71, 40)),
     dict(type="fp8", K=3, B=3, lens=(640, 70, 5), n_q=8, n_kv=1, D=128, window=200, sinks=64, page=64),
     dict(type="f32", K=20, B=2, lens=(400, 64), n_q=4, n_kv=2, D=64, window=33, sinks=3),
+    dict(type="bf16", K=40, B=2, lens=(100, 0), n_q=4, n_kv=1, D=64, window=2**31 - 1, sinks=2**31 - 1),
+    dict(type="bf16", K=400, B=2, lens=(100, 0), n_q=2, n_kv=1, D=64, window=2**31 - 1, tree=5),
     # trees
     dict(type="bf16", K=15, B=3, lens=(100, 0, 63), n_q=8, n_kv=2, D=128, tree=3),
     dict(type="bf16", K=100, B=2, lens=(64, 31), n_q=8, n_kv=1, D=128, tree=20),
