@@ -39,7 +39,7 @@ typedef __attribute__((ext_vector_type(2))) int i32x2;
 
 // DP: head size, padded; WQ x WK x WD waves: WQ blocks of 32 vectors, WK parts of KT tokens of a tile, WD parts of the head size: those waves make the same
 // scores, each for its own part of O.  At DP = 256 all of O for 32 vectors leaves a wave too few registers for its loads' addresses, which then come back
-// from memory between the loads: with WD = 2, 21 windows x 1 row x 8 heads over 5000 tokens of 4 heads take 86 us (5.0 TB/s) instead of 215
+// from memory between the loads: with WD = 2, 21 windows x 1 row x 8 heads over 5000 tokens of 4 heads take 86 us (5.0 TB/s) instead of 215.  Smaller heads gain by more waves to issue loads
 template <CacheType TYPE_, int DP_, int WQ_, int WK_, int KT_, int NST_, int PER_CU_, int WD_ = 1>
 struct Form {
     static constexpr CacheType TYPE = TYPE_;

@@ -3,12 +3,14 @@
 
 namespace aj {
 
+// Few vectors, 32 windows x 1 row x 32 heads over 4000 tokens of 8: heads of 64 take 109 us (4 waves over 128 tokens 119), of 128 333 (four waves over parts of O 388), of 256 757.  Many,
+// 16 windows x 64 rows: heads of 64 150 us (tiles of 64 tokens 155), of 128 285 (tiles of 64, one workgroup per compute unit 301), of 256 709
 template <int DP, bool FEW> struct Choice;
 template <> struct Choice<64, true> { typedef Form<CACHE_F32, 64, 1, 2, 32, 2, 2> F; };
 template <> struct Choice<128, true> { typedef Form<CACHE_F32, 128, 1, 2, 32, 2, 1> F; };
 template <> struct Choice<256, true> { typedef Form<CACHE_F32, 256, 1, 1, 32, 2, 1, 4> F; };
-template <> struct Choice<64, false> { typedef Form<CACHE_F32, 64, 4, 1, 64, 2, 2> F; };
-template <> struct Choice<128, false> { typedef Form<CACHE_F32, 128, 4, 1, 64, 2, 1> F; };
+template <> struct Choice<64, false> { typedef Form<CACHE_F32, 64, 4, 1, 32, 2, 2> F; };
+template <> struct Choice<128, false> { typedef Form<CACHE_F32, 128, 4, 1, 32, 2, 2> F; };
 template <> struct Choice<256, false> { typedef Form<CACHE_F32, 256, 4, 1, 32, 2, 1> F; };
 
 template <int DP>

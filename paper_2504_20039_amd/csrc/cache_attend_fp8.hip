@@ -3,13 +3,15 @@
 
 namespace aj {
 
+// Few vectors, 32 windows x 1 row x 32 heads over 4000 tokens of 8: heads of 64 take 35.5 us (2 waves 41), of 128 55 (4 waves over 128 tokens 59), of 256 98.  Many, 16 windows x 64 rows:
+// heads of 256 107 us (tiles of 32 tokens 114), of 128 57 with two stages and with three
 template <int DP, bool FEW> struct Choice;
 template <> struct Choice<64, true> { typedef Form<CACHE_FP8, 64, 1, 4, 32, 2, 2> F; };
-template <> struct Choice<128, true> { typedef Form<CACHE_FP8, 128, 1, 4, 32, 2, 2> F; };
+template <> struct Choice<128, true> { typedef Form<CACHE_FP8, 128, 1, 2, 32, 2, 2, 2> F; };
 template <> struct Choice<256, true> { typedef Form<CACHE_FP8, 256, 1, 2, 32, 2, 2, 2> F; };
 template <> struct Choice<64, false> { typedef Form<CACHE_FP8, 64, 4, 1, 64, 2, 2> F; };
 template <> struct Choice<128, false> { typedef Form<CACHE_FP8, 128, 4, 1, 64, 2, 2> F; };
-template <> struct Choice<256, false> { typedef Form<CACHE_FP8, 256, 4, 1, 32, 4, 1> F; };
+template <> struct Choice<256, false> { typedef Form<CACHE_FP8, 256, 4, 1, 64, 4, 1> F; };
 
 template <int DP>
 static hipError_t launch(bool few, const AttendArgs &a, hipStream_t s)

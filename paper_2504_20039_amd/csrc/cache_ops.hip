@@ -137,8 +137,9 @@ static hipError_t launch_append(const AppendArgs &a, hipStream_t s)
 {
     const int LG = a.D <= 64 ? 8 : a.D <= 128 ? 16 : 32, per = 256 / LG, passes = (a.n_q + 2 * a.n_kv + per - 1) / per;
     const int rows = a.pages.B * a.pages.rows;
-    // a few rows: one pass per workgroup, for latency; many: one workgroup per row, which makes its cosines once
-    const dim3 grid(rows, rows >= 1024 ? 1 : passes);
+    // a few rows: one pass per workgroup, for latency; many: one workgroup per row, which makes its cosines once (64 + 16 heads of 128: 264 rows 7.6 us in five passes and 9.0
+    // in one workgroup, 1024 rows 13.4 and 14.0, 2048 rows 22.3 and 21.2, 8320 rows 95 and 79)
+    const dim3 grid(rows, rows > 1024 ? 1 : passes);
     if (LG == 8) append_kernel<TYPE, 8><<<grid, 256, 0, s>>>(a);
     else if (LG == 16) append_kernel<TYPE, 16><<<grid, 256, 0, s>>>(a);
     else append_kernel<TYPE, 32><<<grid, 256, 0, s>>>(a);
@@ -216,6 +217,8 @@ __global__ __launch_bounds__(THREADS) void tree_mask_kernel(int rows, const int3
 hipError_t tree_mask(int B, int K, const int32_t *parent, int32_t *depth, uint32_t *mask, hipStream_t s)
 {
     const int rows = K + 1;
+    // words and rows of a thread are known at compile time, and a workgroup is no larger than the tree: the largest form for all would take 24 us instead of 5.5 for 128 trees of 60 nodes, 34
+    // instead of 11.5 for 500
     if (rows <= 64) tree_mask_kernel<64, 64><<<B, 64, 0, s>>>(rows, parent, depth, mask);
     else if (rows <= 128) tree_mask_kernel<128, 256><<<B, 256, 0, s>>>(rows, parent, depth, mask);
     else if (rows <= 256) tree_mask_kernel<256, 512><<<B, 512, 0, s>>>(rows, parent, depth, mask);
