@@ -29,8 +29,8 @@ def _stale(target, deps):
 
 def build(force: bool = False, verbose: bool = False, check: bool = False) -> str:
     """Compile every csrc/*.hip to an object and link them into libaj.so.  check: also verify the generated code of the
-    hand-scheduled kernels (check_isa.py); raises if a loop holds spills, register-file moves or foreign waits, or if a kernel
-    whose tiles use nearly all registers spills any."""
+    hand-scheduled kernels (check_isa.py); raises if a loop holds spills, register-file moves or foreign waits, if a kernel
+    whose tiles use nearly all registers spills any, or if a hand-written load lacks a wait state."""
     from . import check_isa
     os.makedirs(OBJDIR, exist_ok=True)
     headers = glob.glob(os.path.join(CSRC, "*.h")) + [os.path.join(HERE, "..", "include", "aj.h")]
@@ -59,6 +59,7 @@ def build(force: bool = False, verbose: bool = False, check: bool = False) -> st
         run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
     if check:
         check_isa.check_spills("\n".join(reports))
+        check_isa.check_waits(LIB)
         check_isa.check(HIPCC, FLAGS, verbose)
     return LIB
 

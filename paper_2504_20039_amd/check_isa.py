@@ -7,16 +7,21 @@ around those statements: no accumulator moved between the register files, nothin
 toolchain or flag can change that without any error, so the build compiles the two files to assembly text once more and looks at the
 loops.  Of the small tiles, the fp32 tiles on the bf16 instructions and the 256 x 256 tiles
 it looks at what the compiler reports of spilled registers.
+
+The compiler keeps the wait states that the instruction set asks for between its own instructions, but knows nothing of those in
+hand-written statements: the whole library is disassembled and looked over for them (``missing_waits``).
 """
 from __future__ import annotations
 
 import os
 import re
+import struct
 import subprocess
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
+OBJDUMP = os.environ.get("LLVM_OBJDUMP", "/opt/rocm/llvm/bin/llvm-objdump")
 
 
 def _kernels(asm_text):
@@ -184,6 +189,50 @@ def check_spills(report):
             problems.append(f"{name}: {m.group(1)} registers spilled")
     if problems:
         raise RuntimeError("kernels spill registers:\n  " + "\n  ".join(problems))
+
+
+def disassemble(library):
+    """Lines of the gfx950 code in a library built here (the code objects of its offload bundles, one after another)."""
+    data, magic = open(library, "rb").read(), b"__CLANG_OFFLOAD_BUNDLE__"
+    at, lines = data.find(magic), []
+    with tempfile.TemporaryDirectory() as tmp:
+        while at >= 0:
+            n, pos = struct.unpack_from("<Q", data, at + 24)[0], at + 32
+            for _ in range(n):
+                offset, size, name = struct.unpack_from("<QQQ", data, pos)
+                pos += 24 + name
+                if size and data[pos - name:pos].endswith(b"gfx950"):
+                    part = os.path.join(tmp, "code")
+                    with open(part, "wb") as f:
+                        f.write(data[at + offset:at + offset + size])
+                    r = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", "--no-leading-addr", part], check=True, capture_output=True, text=True)
+                    lines += r.stdout.splitlines()
+            at = data.find(magic, at + 24)
+    return lines
+
+
+def missing_waits(lines):
+    """What the code lacks of the wait states that the program has to keep itself: one between a scalar write of M0 and a load whose destination is LDS,
+    at M0 (the load may land where M0 pointed before)."""
+    problems, kernel, m0 = [], "", False
+    for line in lines:
+        m = re.match(r"(?:[0-9a-f]+ )?<?(_Z\w+)>?:", line)
+        if m:
+            kernel, m0 = m.group(1), False
+            continue
+        t = line.split("//")[0].split(";")[0].strip()
+        if not t or t.endswith(":") or t.startswith("."):
+            continue
+        if m0 and re.match(r"(global|buffer|scratch)_load", t) and "lds" in t:
+            problems.append(f"{kernel}: '{t}' directly behind a write of M0")
+        m0 = re.match(r"s_\w+\s+m0\b", t) is not None
+    return problems
+
+
+def check_waits(library):
+    problems = missing_waits(disassemble(library))
+    if problems:
+        raise RuntimeError(f"wait states are missing in {len(problems)} places:\n  " + "\n  ".join(problems[:20]))
 
 
 def check(hipcc, flags, verbose=False):

@@ -32,16 +32,16 @@ __device__ __forceinline__ void load_to_lds_16_nt(const char *base, uint32_t lan
                  : "memory");
 }
 
-// Same load for the hand-scheduled loop: two instructions, M0 not restored (nothing else in these
-// kernels uses M0, and the compiler sets it itself before any use of its own).
+// Same load for the hand-scheduled loop: M0 not restored (nothing else in these kernels uses M0, and the compiler sets it itself before
+// any use of its own).  The s_nop is the wait state that the instruction set asks for between a write of M0 and a load into LDS.
 __device__ __forceinline__ void lds_dma_16(const char *base, uint32_t lane_off, uint32_t lds_dst)
 {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
 }
 
 __device__ __forceinline__ void lds_dma_16_nt(const char *base, uint32_t lane_off, uint32_t lds_dst)
 {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
 }
 
 __device__ __forceinline__ uint32_t lds_offset_of(const void *p)
