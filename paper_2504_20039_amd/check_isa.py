@@ -211,21 +211,46 @@ def disassemble(library):
     return lines
 
 
+def _scalars(text):
+    out = set()
+    for first, last, one in re.findall(r"\bs(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
+        out |= set(range(int(first), int(last) + 1)) if first else {int(one)}
+    return out
+
+
 def missing_waits(lines):
-    """What the code lacks of the wait states that the program has to keep itself: one between a scalar write of M0 and a load whose destination is LDS,
-    at M0 (the load may land where M0 pointed before)."""
-    problems, kernel, m0 = [], "", False
+    """What the code lacks of the wait states that the program has to keep itself:
+
+    * one between a scalar write of M0 and a load whose destination is LDS, at M0 (the load may land where M0 pointed before);
+    * five between a vector instruction that writes a scalar register and a vector memory instruction that reads it (it may read the old value)."""
+    problems, kernel, m0, written = [], "", False, {}      # written: scalar register -> wait states since a vector instruction wrote it
     for line in lines:
         m = re.match(r"(?:[0-9a-f]+ )?<?(_Z\w+)>?:", line)
         if m:
-            kernel, m0 = m.group(1), False
+            kernel, m0, written = m.group(1), False, {}
             continue
         t = line.split("//")[0].split(";")[0].strip()
         if not t or t.endswith(":") or t.startswith("."):
             continue
-        if m0 and re.match(r"(global|buffer|scratch)_load", t) and "lds" in t:
-            problems.append(f"{kernel}: '{t}' directly behind a write of M0")
-        m0 = re.match(r"s_\w+\s+m0\b", t) is not None
+        op, _, operands = t.partition(" ")
+        if re.match(r"(global|buffer|scratch|flat)_", op):
+            if m0 and "lds" in t:
+                problems.append(f"{kernel}: '{t}' directly behind a write of M0")
+            if written and (early := [f"s{r}" for r in _scalars(operands) if written.get(r, 5) < 5]):
+                problems.append(f"{kernel}: '{t}' too soon behind a vector instruction's write of {', '.join(early)}")
+        m0 = op.startswith("s_") and operands.lstrip().startswith("m0,")
+        if written:
+            states = int(operands, 0) + 1 if op == "s_nop" else 1
+            written = {r: n + states for r, n in written.items() if n + states < 5}
+        if op.startswith("v_"):
+            # lanes read, comparisons, and the second result of additions and divisions that have one
+            place = 0 if re.match(r"v_(readlane|readfirstlane|cmp)", op) else 1 if re.match(r"v_(\w*_co_|div_scale|mad_[iu]64)", op) else None
+            if place is not None:
+                for r in _scalars(operands.split(",")[place]):
+                    written[r] = 0
+        elif written and op.startswith("s_") and op not in ("s_nop", "s_waitcnt"):
+            for r in _scalars(operands.split(",")[0]):      # (of a scalar write the hardware knows)
+                written.pop(r, None)
     return problems
 
 

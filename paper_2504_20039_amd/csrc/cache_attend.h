@@ -77,7 +77,7 @@ __device__ __forceinline__ int f_v(int row)
     return F::RB >= 256 ? (row & 3) << 2 | (row >> 2 & 1) << 1 : (row >> 1 & 1) << 2 | (row >> 2 & 1) << 1;
 }
 
-// (s_nop: as in lds_dma_16)
+// (s_nop: the wait state between the write of M0 and a load into LDS)
 __device__ __forceinline__ void load_to_lds_16_at(const char *at, uint32_t lds_dst)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds_dst) : "memory");

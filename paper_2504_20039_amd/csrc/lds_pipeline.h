@@ -10,12 +10,16 @@ namespace aj {
 // LDS read after ALL outstanding loads of this kind (s_waitcnt vmcnt(0)), which would drain the
 // pipeline at every stage.  Here the kernel does its own accounting (wait_vm_and_barrier below); the
 // compiler sees only a memory clobber.  lds_dst must be wave-uniform (it travels in M0).
+// The wait states that the instruction set asks for are kept here, since the compiler does not look into the statement: a vector load reads its
+// scalar base 5 states after a vector instruction wrote it (the compiler brings spilled scalar registers back by v_readlane), so the base
+// goes through a scalar move, for which the hardware waits; and that move is the one state between the write of M0 and the load.
 __device__ __forceinline__ void load_to_lds_16(const char *base, uint32_t lane_off, uint32_t lds_dst)
 {
     // base: wave-uniform global pointer; lane_off: this lane's unsigned byte offset from it
     uint32_t saved_m0;   // M0 is reserved for the compiler: keep its value across the statement
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
-                 : "=&s"(saved_m0)
+    const char *from;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_mov_b64 %1, %3\n\tglobal_load_lds_dwordx4 %2, %1\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0), "=&s"(from)
                  : "v"(lane_off), "s"(base), "s"(lds_dst)
                  : "memory");
 }
@@ -26,22 +30,25 @@ __device__ __forceinline__ void load_to_lds_16(const char *base, uint32_t lane_o
 __device__ __forceinline__ void load_to_lds_16_nt(const char *base, uint32_t lane_off, uint32_t lds_dst)
 {
     uint32_t saved_m0;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b32 m0, %0"
-                 : "=&s"(saved_m0)
+    const char *from;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_mov_b64 %1, %3\n\tglobal_load_lds_dwordx4 %2, %1 nt\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0), "=&s"(from)
                  : "v"(lane_off), "s"(base), "s"(lds_dst)
                  : "memory");
 }
 
 // Same load for the hand-scheduled loop: M0 not restored (nothing else in these kernels uses M0, and the compiler sets it itself before
-// any use of its own).  The s_nop is the wait state that the instruction set asks for between a write of M0 and a load into LDS.
+// any use of its own).
 __device__ __forceinline__ void lds_dma_16(const char *base, uint32_t lane_off, uint32_t lds_dst)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
+    const char *from;
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0" : "=&s"(from) : "v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
 }
 
 __device__ __forceinline__ void lds_dma_16_nt(const char *base, uint32_t lane_off, uint32_t lds_dst)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
+    const char *from;
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0 nt" : "=&s"(from) : "v"(lane_off), "s"(base), "s"(lds_dst) : "memory");
 }
 
 __device__ __forceinline__ uint32_t lds_offset_of(const void *p)

@@ -20,6 +20,18 @@ def test_loads_that_do_not_read_m0():
     assert not check_isa.missing_waits(["s_mov_b32 m0, s33 // 000000002EF4: BEFC0021", "s_endpgm", "0000000000001900 <_Z1kv>:", LOAD])
 
 
+@pytest.mark.parametrize("write", ["v_readlane_b32 s9, v252, 10", "v_readfirstlane_b32 s8, v1", "v_cmp_eq_u32_e64 s[8:9], v1, v2", "v_add_co_u32_e64 v1, s[8:9], v2, v3",
+                                   "v_mad_u64_u32 v[2:3], s[8:9], v4, v5, 0"])
+@pytest.mark.parametrize("between,missing", [([], 1), (["s_nop 3"], 1), (["s_nop 4"], 0), (["s_mov_b32 m0, s3", "s_nop 0"], 1), (["s_waitcnt vmcnt(7)"] * 4, 1),
+                                             (["v_add_u32_e32 v2, v3, v4"] * 5, 0), (["s_nop 1", "s_nop 1", "s_nop 0"], 0)])
+def test_a_base_that_a_vector_instruction_wrote(write, between, missing):
+    assert len(check_isa.missing_waits(["_Z1kv:", write, *between, LOAD])) == missing
+    # of another register, or written once more by a scalar instruction, it is none
+    assert not check_isa.missing_waits([write, *between, "s_nop 0", "global_load_lds_dwordx4 v1, s[10:11]"])
+    assert not check_isa.missing_waits([write, *between, "s_mov_b64 s[8:9], s[4:5]", LOAD])
+    assert not check_isa.missing_waits([write, *between, "_Z2k2v:", LOAD])
+
+
 def test_the_library_keeps_them():
     import paper_2504_20039_amd as aj
     lines = check_isa.disassemble(aj.library_path())
