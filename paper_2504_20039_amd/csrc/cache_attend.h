@@ -738,7 +738,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                     const bool dead = t >= sp.hi || (a.window && t >= a.sinks && t < sp.lo) || pages.gone[page_of(i, row)];
                     u32x4 *at = (u32x4 *)(tile + F::TILE + e * 16);
                     if (dead) *at = u32x4{0, 0, 0, 0};
-                    else if (sp.R > 1) {
+                    else if (sp.R > 1 || a.mask) {      // (a lone row sees what is not dead, unless its mask says otherwise)
                         const u32x4 y = *at;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {

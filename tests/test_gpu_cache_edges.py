@@ -1,0 +1,37 @@
+"""aj_cache_attend where masks, infinities, scales and lengths are at their edges."""
+import copy
+import math
+
+import pytest
+import torch
+
+import cache_ref as ref
+from test_gpu_cache_attend import check, poison, queries, run
+
+pytestmark = pytest.mark.gpu
+NAN8 = 0x7F
+
+
+def put(c, pool, at, x):
+    if c.type == "fp8":
+        c.pools[pool].view(torch.uint8)[at] = NAN8
+    else:
+        c.pools[pool][at] = x
+
+
+@pytest.mark.parametrize("type", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("K,rows", [(0, None), (6, (1, 1, 1, 1)), (6, (1, 7, 1, 3))])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (40, 1, 128), (2, 1, 256), (6, 2, 80)], ids=str)
+def test_a_lone_row_whose_mask_leaves_out_itself(type, K, rows, heads):
+    """One live row, its own bit clear: its slot may hold anything.  It sees the cached tokens, or nothing."""
+    n_q, n_kv, D = heads
+    c = ref.Cache(31, type=type, K=K, B=4, lens=(0, 64, 1, 900), rows=rows, n_q=n_q, n_kv=n_kv, D=D)
+    poison(c)
+    for b, bad in enumerate((math.nan, math.inf, -math.inf, math.nan)):
+        put(c, 0, c.slot(b, c.lens[b]), math.nan)
+        put(c, 1, c.slot(b, c.lens[b]), bad)
+    q = queries(c)
+    kw = dict(scale=D**-0.5, sets=[[set(range(1, r + 1)) for r in range(K + 1)] for _ in range(4)])
+    got, lse = run(c, q, **kw)
+    check(c, q, got, lse, **kw)
+    assert (got[0, 0] == 0).all() and (lse[0, 0] == -math.inf).all()
