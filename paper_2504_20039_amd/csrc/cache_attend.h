@@ -51,6 +51,7 @@ struct Form {
     static constexpr int NI = TILE / 1024 / WAVES;                            // load instructions of a wave for the keys of a tile (values: the same)
     static constexpr int NKB = KT / 32, DB = DP / 32 / WD, QREGS = TYPE == CACHE_F32 ? DP / 8 : DP / 16;
     static constexpr int SEG = 1024;                                          // pages in LDS
+    static constexpr bool ZEROS = TYPE == CACHE_BF16 && DP == 256 && WQ > 1;
     static constexpr int MERGE = WK > 1 ? WQ * WK * DP * 32 * 4 : 0;            // bytes to add up the waves' parts
     static constexpr int LDS = NST * STAGE > MERGE ? NST * STAGE : MERGE;
     static_assert(TILE % (1024 * WAVES) == 0 && CPR <= 64 && 2 * NI * (NST - 1) < 64, "whole load instructions, vmcnt");
@@ -412,7 +413,11 @@ struct Segment {
     uint8_t gone[F::SEG];
 };
 
-template <class F>
+// PADDED: the head size is below DP.  What the loads put behind a key are copies of its first elements, which must not count: an infinity among them times the
+// query's zero is no number.  Steps of the scores that lie there are left out, or (ZEROS) take zeros for the keys: 32 windows x 1 row over 4000 tokens in fp32, heads of
+// 208: 690 us, with all steps 756; 16 windows x 64 rows over 1000 tokens in bf16, heads of 240: 72 us with zeros, 76 with steps left out, whose branches make that
+// form spill.  (FP8 has no infinities, and its heads may end inside a step)
+template <class F, bool PADDED>
 __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PER_CU *F::WAVES / 4) void attend_kernel(AttendArgs a)
 {
     constexpr int ST = F::ST, RB = F::RB, KT = F::KT, DB = F::DB, NKB = F::NKB, NI = F::NI, QB = F::QB, NST = F::NST;
@@ -422,6 +427,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
     __shared__ int sums[F::WAVES], found[4];
     __shared__ int wflag[2][F::WAVES];
     __shared__ float mls[2][F::WK][QB];
+    __shared__ u32x4 zero;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
     const int wq = wave % F::WQ, wk = wave / F::WQ % F::WK, wd = wave / (F::WQ * F::WK), db0 = wd * DB;      // db0: the wave's first 32 elements of O
@@ -432,6 +438,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
     const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, per_xcd = a.clusters / 8;
     const int members = a.heads * a.blocks, cluster = uniform(xcd * per_xcd + place / members), member = uniform(place % members);
     const int block = uniform(member % a.blocks), head_of_group = uniform(member / a.blocks);
+    if (PADDED && F::ZEROS && tid == 0) zero = u32x4{0, 0, 0, 0};      // (there are barriers before it is read)
     Line<ST, F::THREADS> line;
     if (!line.begin(a, cluster, a.clusters, sums, found)) return;
     const int total = line.total, cuts = line.cuts, w_end = line.w_end;
@@ -449,7 +456,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
     for (int n = 0; n < NI; ++n) {
         const int row = (wave * NI + n) * F::RPI + lane / F::CPR, pc = lane % F::CPR;
         int ck = pc ^ f_k<F>(row), cv = pc ^ f_v<F>(row);
-        if (ck * 16 >= a.D * F::KES) ck = 0;      // padding: the query is zero there, and what comes of the values is not written
+        if (ck * 16 >= a.D * F::KES) ck = 0;      // padding: the scores leave it out, and what comes of the values is not written
         if (cv * 16 >= a.D * F::KES) cv = 0;
         k_off[n] = (uint32_t)(row & (page - 1)) * slot_stride + ck * 16;
         v_off[n] = (uint32_t)(row & (page - 1)) * slot_stride + cv * 16;
@@ -597,15 +604,23 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                 // would take more registers than there are
                 constexpr int KS = RB / 32, AHEAD = 2;
                 u32x4 y[AHEAD + 1][NKB];
+                // whether step ks lies behind the head (which is longer than half of DP, or the smaller form has it, and comes in steps of 16 elements)
+                const auto behind = [&](int ks) ALWAYS_INLINE {
+                    return PADDED && (F::DP == 64 || 2 * ks >= KS) && 32 * ks % (16 * F::KES) == 0 && 32 * ks >= a.D * F::KES;
+                };
                 const auto ask = [&](int ks) ALWAYS_INLINE {
 #pragma unroll
-                    for (int kb = 0; kb < NKB; ++kb) y[ks % (AHEAD + 1)][kb] = from_lds<u32x4>((base ^ (32 * ks)) + kb * 32 * RB);
+                    for (int kb = 0; kb < NKB; ++kb) {
+                        const uint32_t at = (base ^ (32 * ks)) + kb * 32 * RB;
+                        y[ks % (AHEAD + 1)][kb] = from_lds<u32x4>(F::ZEROS && behind(ks) ? lds_offset_of(&zero) : at);
+                    }
                 };
 #pragma unroll
                 for (int ks = 0; ks < AHEAD && ks < KS; ++ks) ask(ks);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
+                    if (!F::ZEROS && behind(ks)) break;
                     if (ks + AHEAD < KS) ask(ks + AHEAD);
 #pragma unroll
                     for (int kb = 0; kb < NKB; ++kb) {
@@ -920,7 +935,9 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 template <class F>
 hipError_t launch_attend(const AttendArgs &a, hipStream_t s)
 {
-    attend_kernel<F><<<a.clusters * a.heads * a.blocks, F::THREADS, 0, s>>>(a);
+    constexpr bool CAN_PAD = F::TYPE != CACHE_FP8;
+    if (CAN_PAD && a.D < F::DP) attend_kernel<F, CAN_PAD><<<a.clusters * a.heads * a.blocks, F::THREADS, 0, s>>>(a);
+    else attend_kernel<F, false><<<a.clusters * a.heads * a.blocks, F::THREADS, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -35,3 +35,20 @@ def test_a_lone_row_whose_mask_leaves_out_itself(type, K, rows, heads):
     got, lse = run(c, q, **kw)
     check(c, q, got, lse, **kw)
     assert (got[0, 0] == 0).all() and (lse[0, 0] == -math.inf).all()
+
+
+@pytest.mark.parametrize("type", ["bf16", "f32"])
+@pytest.mark.parametrize("K,lens", [(0, (70, 1500)), (40, (70, 500))])
+@pytest.mark.parametrize("D", [16, 48, 64, 80, 112, 128, 144, 208, 256])
+def test_infinite_keys_whose_weight_is_zero(type, K, lens, D):
+    """A score of -infinity is a weight of zero at every head size: as if the token were nowhere."""
+    c = ref.Cache(32, type=type, K=K, B=2, lens=lens, n_q=4, n_kv=1, D=D, page=1)
+    q = queries(c)
+    q[..., 0], q[..., D - 1] = q[..., 0].abs() + 0.5, q[..., D - 1].abs() + 0.5
+    without = copy.copy(c)
+    without.table = c.table.clone()
+    for b, t, e in ((0, 3, 0), (0, 66, D - 1), (1, lens[1] // 2, 0), (1, lens[1] - 1, D - 1)):
+        c.pools[0][c.slot(b, t)][:, e] = -math.inf
+        without.table[b, t] = -1
+    got, lse = run(c, q, scale=0.1)
+    check(without, q, got, lse, scale=0.1)
