@@ -338,7 +338,7 @@ int aj_cache_append(aj_cache *c, const void *q, const void *k, const void *v, co
  * Attention of the new rows over the cache, which holds the new rows themselves already (aj_cache_append):
  *     s[t] = scale * q . (k_scale * k_pool[t]),  out = sum_t softmax(s)[t] * (v_scale * v_pool[t]),  lse = log sum_t exp(s[t])
  * over the tokens t that row r sees: cached tokens, and new rows by `mask` or up to itself; of these, with a window, those at positions above
- * position(r) - window or below sinks.  A row that sees nothing gives out = 0 and lse = -inf.
+ * position(r) - window or below sinks.  A row that sees nothing, or whose scores are all -inf, gives out = 0 and lse = -inf.
  *   q   [B][K+1][n_q][head_dim]   rows q_stride apart
  *   out [B][K+1][n_q][head_dim]   dense;   lse [B][K+1][n_q] float or NULL.  Neither overlaps what the call reads
  * Scores, their maxima and sums and the weighted sums are held in fp32; with bf16 the weights are rounded to bf16 before they meet the

@@ -346,13 +346,15 @@ template <CacheType TYPE>
 __device__ __forceinline__ void finish(const AttendArgs &a, int64_t vec, int d4, f32x4 o, float l)
 {
     if (4 * d4 >= a.D) return;
-    const float f = l > 0.f || l != l ? a.v_scale / l : 0.f;
+    const float f = a.v_scale / l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = l == 0.f ? 0.f : o[i] * f;      // (a sum of zeros times values that are not finite is no number)
     if constexpr (TYPE == CACHE_F32) {
-        *(f32x4 *)((float *)a.out + vec * a.D + 4 * d4) = f32x4{o[0] * f, o[1] * f, o[2] * f, o[3] * f};
+        *(f32x4 *)((float *)a.out + vec * a.D + 4 * d4) = o;
     } else {
         bf16x4 y;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = (__bf16)(o[i] * f);
+        for (int i = 0; i < 4; ++i) y[i] = (__bf16)o[i];
         *(bf16x4 *)((__bf16 *)a.out + vec * a.D + 4 * d4) = y;
     }
 }

@@ -52,3 +52,17 @@ def test_infinite_keys_whose_weight_is_zero(type, K, lens, D):
         without.table[b, t] = -1
     got, lse = run(c, q, scale=0.1)
     check(without, q, got, lse, scale=0.1)
+
+
+@pytest.mark.parametrize("type", ["bf16", "f32"])
+@pytest.mark.parametrize("K,lens", [(0, (70, 1500)), (40, (70, 500))])
+@pytest.mark.parametrize("D", [64, 80, 256])
+def test_rows_whose_scores_are_all_minus_infinity(type, K, lens, D):
+    """Nothing has any weight: zeros, whatever the values are."""
+    c = ref.Cache(34, type=type, K=K, B=2, lens=lens, n_q=4, n_kv=1, D=D)
+    q = queries(c)
+    q[..., 1] = q[..., 1].abs() + 0.5
+    c.pools[0][..., 1] = -math.inf
+    c.pools[1][c.slot(0, 5)], c.pools[1][c.slot(1, lens[1])] = math.inf, math.nan
+    got, lse = run(c, q, scale=0.1)
+    assert (got == 0).all() and (lse == -math.inf).all()
