@@ -342,7 +342,8 @@ int aj_cache_append(aj_cache *c, const void *q, const void *k, const void *v, co
  *   q   [B][K+1][n_q][head_dim]   rows q_stride apart
  *   out [B][K+1][n_q][head_dim]   dense;   lse [B][K+1][n_q] float or NULL.  Neither overlaps what the call reads
  * Scores, their maxima and sums and the weighted sums are held in fp32; with bf16 the weights are rounded to bf16 before they meet the
- * values.  The same call gives the same bits.  Errors as aj_cache_append, and AJ_EINVAL unless scale * k_scale is positive and finite.
+ * values.  q . k_pool itself is a sum in fp32, before the scales.  The same call gives the same bits.  Errors as aj_cache_append, and AJ_EINVAL
+ * unless scale is positive and scale * k_scale * log2(e) is a normal number of fp32 (2^-126 .. 2^128).
  */
 int aj_cache_attend(aj_cache *c, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table, const int32_t *cache_len,
                     const int32_t *n_rows, const int32_t *depth, const uint32_t *mask, float scale, float k_scale, float v_scale,

@@ -20,6 +20,7 @@
 // time).  Every workgroup finds its piece by a prefix sum over the windows.  Items cut by a piece's border leave partial results (maximum, sum,
 // unscaled O in fp32), which the last workgroup to arrive adds in the order of the pieces, so that the same call gives the same bits.
 #pragma once
+#include <float.h>
 #include <math.h>
 
 #include "cache.h"
@@ -448,7 +449,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
     Span sp = span_of<ST>(a, line.L, line.R);
 
     const uint32_t lds0 = lds_offset_of(lds);
-    const float c = a.score_scale, threshold = 8.f / c;
+    const float c = a.score_scale, threshold = fminf(8.f / c, FLT_MAX);      // (infinite, nothing would exceed -infinity by it)
     const int per_tile = page < ST ? ST >> a.pages.log_page : 1, seg_tiles = F::SEG / per_tile;
     const bool once = a.blocks == 1;
     const uint32_t slot_stride = (uint32_t)a.pages.slot_stride;

@@ -66,3 +66,19 @@ def test_rows_whose_scores_are_all_minus_infinity(type, K, lens, D):
     c.pools[1][c.slot(0, 5)], c.pools[1][c.slot(1, lens[1])] = math.inf, math.nan
     got, lse = run(c, q, scale=0.1)
     assert (got == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("type,scale", [("bf16", 1.6e-38), ("f32", 0.9e-38), ("f32", 1.6e-38), ("fp8", 5e-37)])
+@pytest.mark.parametrize("K,lens", [(0, (3000, 20)), (40, (700, 0))])
+@pytest.mark.parametrize("D", [64, 256])
+def test_the_smallest_scales(type, scale, K, lens, D):
+    """Scales at the lower end of the normal numbers: nearly equal weights, and others with large queries and keys.
+
+    (The sums q . k themselves are held in fp32: here 2^118 times sums of D products of deviation 2, up to 6 times 2 sqrt(D) <= 2^7.6 in all.)"""
+    c = ref.Cache(33, type=type, K=K, B=2, lens=lens, n_q=4, n_kv=2, D=D)
+    q = queries(c)
+    check(c, q, *run(c, q, scale=scale), scale=scale)
+    if type != "fp8":
+        q *= 2.0**58
+        c.pools[0] *= 2.0**60
+        check(c, q, *run(c, q, scale=scale), scale=scale)
