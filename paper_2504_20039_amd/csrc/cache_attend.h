@@ -449,7 +449,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
     Span sp = span_of<ST>(a, line.L, line.R);
 
     const uint32_t lds0 = lds_offset_of(lds);
-    const float c = a.score_scale, threshold = fminf(8.f / c, FLT_MAX);      // (infinite, nothing would exceed -infinity by it)
+    const float c = a.score_scale, threshold = __int_as_float(uniform(__float_as_int(fminf(8.f / c, FLT_MAX))));      // (infinite, nothing would exceed -infinity by it)
     const int per_tile = page < ST ? ST >> a.pages.log_page : 1, seg_tiles = F::SEG / per_tile;
     const bool once = a.blocks == 1;
     const uint32_t slot_stride = (uint32_t)a.pages.slot_stride;
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
         f32x16 acc[DB];
 #pragma unroll
         for (int i = 0; i < DB; ++i) acc[i] = f32x16{0};
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f, over = 0.f;      // over: what l holds too much
 
         const char *k_head = uniform((const char *)a.k_pool + kvh * a.pages.head_stride), *v_head = uniform((const char *)a.v_pool + kvh * a.pages.head_stride);
         const auto tile_of_visit = [&](int i) ALWAYS_INLINE { return i < sp.ns ? i : sp.first + i - sp.ns; };
@@ -657,33 +657,51 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 #pragma unroll
                         for (int e = 0; e < 16; ++e) acc[i][e] *= f;
                     l *= f;
+                    over *= f;
                     m = mn;
                 }
                 const float base = m == -INFINITY ? 0.f : m * c;
+                float sum = 0.f;
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c, -base));
-                        l += s[kb][e];
+                        sum += s[kb][e];
                     }
                 }
+                // Additions of nearly equal terms to a long sum round the same way until its exponent changes: 65536 weights of 0.7 one after another are 6 10^-4
+                // off.  So a tile's weights are added up by themselves, and what adding them to l rounds away goes into the next addition
+                const float more = sum - over, to = l + more;
+                over = to - l - more;
+                l = to;
             };
             // O^T += V^T P^T
             const auto add = [&](uint32_t vt) ALWAYS_INLINE {
                 if constexpr (F32) {
                     const uint32_t base = (vt + here(4 * h * RB + ((col >> 2) ^ (h << 3)) * 16 + (col & 3) * 4)) ^ (128 * db0);
+                    // DG blocks of 32 elements at a time.  A tile's products are added up by themselves too: one takes two tokens (in the other types 16, and the result is
+                    // rounded to 2^-8)
+                    constexpr int DG = F::WQ > 1 && DB > 2 ? 2 : DB;
 #pragma unroll
-                    for (int kb = 0; kb < NKB; ++kb)
+                    for (int d0 = 0; d0 < DB; d0 += DG) {
+                        f32x16 o[DG];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float y[DB];
+                        for (int j = 0; j < DG; ++j) o[j] = f32x16{0};
 #pragma unroll
-                            for (int db = 0; db < DB; ++db)
-                                y[db] = from_lds<float>((base ^ (128 * db)) + (kb * 32 + e % 4 + 8 * (e / 4)) * RB);
+                        for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                            for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[db], s[kb][e], acc[db], 0, 0, 0);
-                        }
+                            for (int e = 0; e < 16; ++e)
+#pragma unroll
+                                for (int j = 0; j < DG; ++j) {
+                                    const float y = from_lds<float>((base ^ (128 * (d0 + j))) + (kb * 32 + e % 4 + 8 * (e / 4)) * RB);
+                                    o[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(y, s[kb][e], o[j], 0, 0, 0);
+                                }
+#pragma unroll
+                        for (int j = 0; j < DG; ++j)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) acc[d0 + j][e] += o[j][e];
+                    }
                 } else {
                     // DG blocks of 32 elements at a time: their fragments are asked for while the products before them run
                     constexpr int KS = KT / 16, DG = DB < 4 ? DB : 4, STEPS = KS * DB / DG;

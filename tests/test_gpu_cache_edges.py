@@ -82,3 +82,35 @@ def test_the_smallest_scales(type, scale, K, lens, D):
         q *= 2.0**58
         c.pools[0] *= 2.0**60
         check(c, q, *run(c, q, scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("weight", [0.7, 0.9])
+@pytest.mark.parametrize("D,G", [(16, 1), (64, 40), (128, 1), (256, 1)])
+def test_long_sums_of_equal_weights(weight, D, G):
+    """An uncut item of 131072 tokens in fp32, all but a few of the same weight: sums that take one token at a time drift by 2 10^-4, since in a binade every addition rounds
+    the same way.
+
+    A lane's part of the sum: at most 64 weights of a tile, one after another, and tiles with what their additions lost; the weights' argument and exponential:
+    within 4 steps; then the logarithm as in the reference: 80 2^-24.  Values: products of a tile one after another, then 2048 or 4096 tiles,
+    each addition off by half a step: (tiles / 2 + 80) 2^-24 of the values' size."""
+    import paper_2504_20039_amd as aj
+    n, page, B = 1 << 17, 1 << 16, 512
+    g = torch.Generator().manual_seed(5)
+    k = torch.zeros(3, page, 1, D)
+    k[..., 0] = math.log(weight)
+    k[0, :128, :, 0] = 0.0
+    v = 0.5 + torch.rand(3, page, 1, D, generator=g)
+    v[..., 1] = 1.0
+    q = torch.zeros(B, 1, G, D)
+    q[..., 0] = 1.0
+    h = aj.aj_cache_create(B, 0, G, 1, D, page, 3, 3, aj.AJ_F32)
+    table = torch.tensor([[0, 1, 2]], dtype=torch.int32).expand(B, 3).contiguous().cuda()
+    out, lse = torch.empty(B, 1, G * D, device="cuda"), torch.empty(B, 1, G, device="cuda")
+    aj.aj_cache_attend(h, q.flatten(2).cuda(), k.cuda(), v.cuda(), table, torch.full((B,), n - 1, dtype=torch.int32, device="cuda"), 1.0, out, lse=lse)
+    torch.cuda.synchronize()
+    aj.aj_cache_destroy(h)
+    w = torch.exp(k.flatten(0, 1)[:n, 0, 0].double())
+    want_lse, want = w.sum().log(), (w[:, None] * v.flatten(0, 1)[:n, 0].double()).sum(0) / w.sum()
+    assert ((lse.double().cpu() - want_lse).abs() <= 80 * 2.0**-24 + 2.0**-22 * want_lse).all(), (lse.double().cpu() - want_lse).abs().max().item()
+    err = (out.double().cpu().view(B, G, D) / want - 1).abs().max().item()
+    assert err <= (n / 32 / 2 + 80) * 2.0**-24, err
