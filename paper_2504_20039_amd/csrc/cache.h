@@ -77,7 +77,6 @@ struct AttendArgs {
     int *arrived;          // [clusters][heads][blocks], zero between calls
 };
 struct AttendPlan {
-    int vectors, tokens;   // query vectors (rows x query heads of one head of keys) of a workgroup, tokens of a tile
     int blocks, heads, clusters;
     size_t parts, part_size;   // partial results, one per vector, and their floats
 };

@@ -285,7 +285,7 @@ extern "C" int aj_cache_commit(aj_cache *h, const uint32_t *mask, const int32_t 
     a.n_layers = n_layers;
     a.n_kv = c.n_kv;
     a.row_bytes = c.head_dim * h->kv_es;
-    a.layer_stride = layer_stride * h->kv_es;
+    a.layer_stride = n_layers > 1 ? layer_stride * h->kv_es : 0;
     a.new_len = new_len;
     const hipError_t e = cache_commit(a, (hipStream_t)stream);
     return e == hipSuccess ? AJ_OK : hip_fail(e);

@@ -966,8 +966,6 @@ template <class F>
 AttendPlan plan_attend(int vectors, int n_kv, int num_cus)
 {
     AttendPlan p;
-    p.vectors = F::QB;
-    p.tokens = F::ST;
     p.blocks = (vectors + F::QB - 1) / F::QB;
     const int places = num_cus / 8 * F::PER_CU;      // of an XCD
     p.heads = 1;

@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
         turn[threadIdx.x] = t;
     }
     __syncthreads();
-    const int64_t slot = (int64_t)L + r < 0x7fffffff ? slot_offset(a.pages, b, L + r) : -1;
+    const int64_t slot = slot_offset(a.pages, b, L + r);
     const int group = threadIdx.x / LG, lane = threadIdx.x % LG, e0 = 8 * lane;
     const bool in = e0 < a.D;
     const int heads = a.n_q + 2 * a.n_kv;
@@ -249,9 +249,8 @@ __global__ __launch_bounds__(256) void commit_kernel(CommitArgs a)
         const int r = 32 * w + tid;
         if (tid < 32 && x >> tid & 1) {
             const int i = n + __popc(x & ((1u << tid) - 1u));
-            // (the path's rows reach no further than K behind L)
-            to[i] = (int64_t)L + i < 0x7fffffff ? slot_offset(a.pages, b, L + i) : -1;
-            of[i] = (int64_t)L + r < 0x7fffffff ? slot_offset(a.pages, b, L + r) : -1;
+            to[i] = slot_offset(a.pages, b, L + i);      // (the path's rows reach no further than K behind L)
+            of[i] = slot_offset(a.pages, b, L + r);
         }
         n += __popc(x);
     }
