@@ -312,7 +312,9 @@ typedef struct {
 } aj_cache_config;
 
 /* Validate cfg, allocate the workspace of aj_cache_attend on the current device.  *out is NULL on failure.  A handle does not own the pools:
-   one handle serves all layers of a model.  As with aj_handle, one call in flight per handle. */
+   one handle serves all layers of a model.  As with aj_handle, one call in flight per handle.  The workspace holds partial results: at heads of 128
+   about 17 MB for up to 32 vectors, (K+1) * n_q / n_kv of them, 68 MB up to 8192, then 8.3 KB a vector; in proportion for heads of up to 64 and 256
+   (17 GB at the limits of all three).  AJ_ENOMEM if there is none. */
 int aj_cache_create(const aj_cache_config *cfg, aj_cache **out);
 
 /* Frees the workspace.  The caller must have synchronised any stream still using the handle. */

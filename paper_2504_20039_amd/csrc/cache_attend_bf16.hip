@@ -5,8 +5,8 @@ namespace aj {
 
 // Few vectors: tiles of 64 tokens, so that two workgroups' stages fit a compute unit up to heads of 128, and waves enough for the issue of their loads.  32 windows x 1 row x
 // 32 heads over 4000 tokens of 8: heads of 64 take 53 us (4 waves over 128 tokens 58), of 128 95 (2 waves with all of O 98, 4 with a quarter of O each over tiles of 32 tokens 102), of 256 166 (4 waves 180)
-// Many: a wave has 32 vectors, two workgroups per compute unit up to heads of 128; 16 windows x 64 rows: heads of 128 63 us (tiles of 32 tokens 60, but 840 and 860 for 128 windows
-// x 65 rows with two and four stages of them, no less than 840), of 256 117 (tiles of 64 149)
+// Many: a wave has 32 vectors, two workgroups per compute unit up to heads of 128; 16 windows x 64 rows x 32 heads over 2000 tokens of 8: heads of 128 61 us (tiles of 32 tokens 60, but 840 and 860 for 128 windows
+// x 65 rows with two and four stages of them, no less than 840), of 256 116 (tiles of 64 149)
 template <int DP, bool FEW> struct Choice;
 template <> struct Choice<64, true> { typedef Form<CACHE_BF16, 64, 1, 2, 32, 2, 2, 2> F; };
 template <> struct Choice<128, true> { typedef Form<CACHE_BF16, 128, 1, 2, 32, 2, 2, 2> F; };

@@ -3,8 +3,9 @@
 
 namespace aj {
 
-// Few vectors, 32 windows x 1 row x 32 heads over 4000 tokens of 8: heads of 64 take 109 us (4 waves over 128 tokens 119), of 128 333 (four waves over parts of O 388), of 256 757.  Many,
-// 16 windows x 64 rows: heads of 64 150 us (tiles of 64 tokens 155), of 128 285 (tiles of 64, one workgroup per compute unit 301), of 256 709
+// Few vectors, 32 windows x 1 row x 32 heads over 4000 tokens of 8: heads of 64 take 112 us (4 waves over 128 tokens 134), of 128 341 (four waves over parts of O 392), of 256 757 (two
+// waves 906).  Many, 16 windows x 64 rows x 32 heads over 2000 tokens of 8: heads of 64 156 us (tiles of 64 tokens 157, over 1000 tokens 93 instead of 88), of 128 290 (tiles of 64, one
+// workgroup per compute unit 306), of 256 628 (64 vectors, two waves over parts of O 915)
 template <int DP, bool FEW> struct Choice;
 template <> struct Choice<64, true> { typedef Form<CACHE_F32, 64, 1, 2, 32, 2, 2> F; };
 template <> struct Choice<128, true> { typedef Form<CACHE_F32, 128, 1, 2, 32, 2, 1> F; };

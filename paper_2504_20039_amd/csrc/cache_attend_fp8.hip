@@ -3,7 +3,7 @@
 
 namespace aj {
 
-// Few vectors, 32 windows x 1 row x 32 heads over 4000 tokens of 8: heads of 64 take 35.5 us (2 waves 41), of 128 55 (4 waves over 128 tokens 59), of 256 98.  Many, 16 windows x 64 rows:
+// Few vectors, 32 windows x 1 row x 32 heads over 4000 tokens of 8: heads of 64 take 35.5 us (2 waves 41), of 128 55 (4 waves over 128 tokens 59), of 256 98.  Many, 16 windows x 64 rows x 32 heads over 2000 tokens of 8:
 // heads of 256 107 us (tiles of 32 tokens 114), of 128 57 with two stages and with three
 template <int DP, bool FEW> struct Choice;
 template <> struct Choice<64, true> { typedef Form<CACHE_FP8, 64, 1, 4, 32, 2, 2> F; };
