@@ -284,8 +284,9 @@ struct Line {
         const float n = (float)total / items;
         const int least = uniform((int)(n <= a.whole ? ceilf(n) : sqrtf(n * a.part_cost))), most = uniform(total / (least < 1 ? 1 : least));
         cuts = most < 1 ? 1 : most < clusters ? most : clusters;
-        // As many pieces to every item of a batch of equal ones, where that makes the pieces longer by less than a second item's start and join take: 44 x 38
-        // rows x 4 heads over 1000 tokens 47 -> 33 us
+        // As many pieces to every item of a batch of equal ones, where that makes the pieces longer by less than a second item's start and join take, about four
+        // tiles: 44 x 38 rows x 4 heads over 1000 tokens 45 -> 33 us.  (One tile: 100 x 38 rows over 700 44 instead of 39.5; sixteen: 33 x 1 row x 32 heads over 700 33 instead of
+        // 29.5)
         const int even = cuts > items ? cuts - cuts % items : cuts;
         if (uniform((int)((float)total * (cuts - even) <= 4.f * even * cuts))) cuts = even;
         if (cluster >= cuts) return false;
@@ -657,7 +658,7 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
 #pragma unroll
                         for (int e = 0; e < 16; ++e) acc[i][e] *= f;
                     l *= f;
-                    over *= f;
+                    if (F32) over *= f;
                     m = mn;
                 }
                 const float base = m == -INFINITY ? 0.f : m * c;
@@ -670,18 +671,23 @@ __global__ __launch_bounds__(F::THREADS, F::PER_CU *F::WAVES / 4 < 1 ? 1 : F::PE
                         sum += s[kb][e];
                     }
                 }
-                // Additions of nearly equal terms to a long sum round the same way until its exponent changes: 65536 weights of 0.7 one after another are 6 10^-4
-                // off.  So a tile's weights are added up by themselves, and what adding them to l rounds away goes into the next addition
-                const float more = sum - over, to = l + more;
-                over = to - l - more;
-                l = to;
+                // Additions of nearly equal terms to a long sum round the same way until its exponent changes: over 131072 tokens of weight 0.7 or 0.9, one after another, sums
+                // are 6 10^-4 off.  So a tile's weights are added up by themselves; and in fp32 what adding them to l rounds away goes into the next addition: 10^-6.  (Results of
+                // 16 bits need no more than the former, some 10^-5, and the latter takes up to 6 % there, heads of 256 and 64 rows)
+                if constexpr (F32) {
+                    const float more = sum - over, to = l + more;
+                    over = to - l - more;
+                    l = to;
+                } else {
+                    l += sum;
+                }
             };
             // O^T += V^T P^T
             const auto add = [&](uint32_t vt) ALWAYS_INLINE {
                 if constexpr (F32) {
                     const uint32_t base = (vt + here(4 * h * RB + ((col >> 2) ^ (h << 3)) * 16 + (col & 3) * 4)) ^ (128 * db0);
-                    // DG blocks of 32 elements at a time.  A tile's products are added up by themselves too: one takes two tokens (in the other types 16, and the result is
-                    // rounded to 2^-8)
+                    // DG blocks of 32 elements at a time.  A tile's products are added up by themselves too, since one takes two tokens: 4 10^-5 for a value that all those
+                    // tokens share, 10^-3 otherwise (in the other types one takes 16, and the result is rounded to 2^-8)
                     constexpr int DG = F::WQ > 1 && DB > 2 ? 2 : DB;
 #pragma unroll
                     for (int d0 = 0; d0 < DB; d0 += DG) {
@@ -968,6 +974,8 @@ AttendPlan plan_attend(int vectors, int n_kv, int num_cus)
     AttendPlan p;
     p.blocks = (vectors + F::QB - 1) / F::QB;
     const int places = num_cus / 8 * F::PER_CU;      // of an XCD
+    // as many heads of a window as leave a tenth of the places unused at most: 128 windows x 65 rows x 64 heads over 1000 tokens take 480 us, one head at a time 486, with up to
+    // half of the places unused 655; one row at a time within 1.5 % either way
     p.heads = 1;
     for (int h = 2; h <= n_kv; ++h)
         if (n_kv % h == 0 && places / (h * p.blocks) * h * p.blocks * 10 >= places * 9) p.heads = h;

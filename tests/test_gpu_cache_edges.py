@@ -114,3 +114,31 @@ def test_long_sums_of_equal_weights(weight, D, G):
     assert ((lse.double().cpu() - want_lse).abs() <= 80 * 2.0**-24 + 2.0**-22 * want_lse).all(), (lse.double().cpu() - want_lse).abs().max().item()
     err = (out.double().cpu().view(B, G, D) / want - 1).abs().max().item()
     assert err <= (n / 32 / 2 + 80) * 2.0**-24, err
+
+
+@pytest.mark.parametrize("type", ["bf16", "fp8"])
+@pytest.mark.parametrize("D,G", [(16, 1), (64, 40), (128, 1), (128, 40), (256, 1), (256, 40)])
+def test_long_sums_of_equal_weights_in_16_bits(type, D, G):
+    """As above: a lane adds at most 2048 tiles, each addition off by half a step, to sums of at most 64 weights.  The weight and the result are rounded to bf16, half a step
+    each."""
+    import paper_2504_20039_amd as aj
+    n, page, B = 1 << 17, 1 << 16, 512
+    g = torch.Generator().manual_seed(6)
+    kv = ref.TYPES[type][1]
+    k = torch.zeros(3, page, 1, D)
+    k[..., 0] = math.log(0.7)
+    k[0, :128, :, 0] = 0.0
+    k, v = k.to(kv), (0.5 + torch.rand(3, page, 1, D, generator=g)).to(kv)
+    q = torch.zeros(B, 1, G, D, dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    h = aj.aj_cache_create(B, 0, G, 1, D, page, 3, 3, aj.AJ_BF16, aj.AJ_KV_FP8_E4M3 if type == "fp8" else aj.AJ_KV_SAME)
+    table = torch.tensor([[0, 1, 2]], dtype=torch.int32).expand(B, 3).contiguous().cuda()
+    out, lse = torch.empty(B, 1, G * D, dtype=torch.bfloat16, device="cuda"), torch.empty(B, 1, G, device="cuda")
+    aj.aj_cache_attend(h, q.flatten(2).cuda(), k.cuda(), v.cuda(), table, torch.full((B,), n - 1, dtype=torch.int32, device="cuda"), 1.0, out, lse=lse)
+    torch.cuda.synchronize()
+    aj.aj_cache_destroy(h)
+    k, v = (x.float().double().flatten(0, 1)[:n, 0] for x in (k, v))
+    w = torch.exp(k[:, 0])
+    want_lse, want = w.sum().log(), (w[:, None] * v).sum(0) / w.sum()
+    assert ((lse.double().cpu() - want_lse).abs() <= (2048 / 2 + 80) * 2.0**-24 + 2.0**-22 * want_lse).all(), (lse.double().cpu() - want_lse).abs().max().item()
+    assert (out.double().cpu().view(B, G, D) / want - 1).abs().max().item() <= 2.0**-7 * 1.01
